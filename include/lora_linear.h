@@ -315,6 +315,153 @@ lora_status lora_linear_group_bwd(const lora_bf16* const* dY, const lora_bf16* X
                                   int64_t m, int64_t k, int64_t r, float alpha, void* stream);
 
 /*
+ * ---- Operators around the layer's output -------------------------------------
+ * A fine-tuned model's weights held in 4 bits, the log probabilities of tokens
+ * under its logits, and distillation from a teacher's top logits.  The
+ * conventions above hold for them; logits may be of any width, pitch and
+ * alignment, and arrays of values or lists per row need the alignment of their
+ * 4-byte type alone.
+ */
+
+/*
+ * Microscaled 4-bit floating point (the MXFP4 format of the OCP Microscaling
+ * Formats specification).  The rows of a matrix [rows, k] are cut into blocks
+ * of 32 columns (the last one may be shorter).  Block b of row i has one scale
+ * 2^(s - 127), s a byte: the exponent of the block's largest magnitude less 2,
+ * at least 0; 255, which stands for NaN, where the block holds a NaN or an
+ * infinity.  An element is its value divided by the scale and rounded to the
+ * nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to the even code, beyond 6 to 6:
+ * a code of 3 bits, and its sign above it.
+ *
+ *   codes   rows of 128 ceil(k/256) bytes; column 2j of a row is the low half
+ *           of byte j, column 2j + 1 the high one; zero beyond column k
+ *   scales  cells of 512 bytes, one per 64 rows and 256 columns: the scale of
+ *           row i, block b is byte ((b/8) G + i/64) 512 + (b%4) 128 + (i%16) 8 +
+ *           (i/16%4) 2 + (b/4%2) (whole-number quotients), G = ceil(rows/64); a
+ *           lane of a matrix product so finds the scales of four rows 16 apart
+ *           and two blocks 4 apart in 8 bytes.  Zero for the rows and blocks
+ *           of a cell beyond the matrix.
+ * rows >= 1, k >= 8 and a multiple of 8 (LORA_ERR_SHAPE), rows x 256
+ * ceil(k/256) at most 2^30 (LORA_ERR_UNSUPPORTED).  The sizes are in bytes, 0 on
+ * invalid arguments.
+ */
+size_t lora_mx4_codes_size(int64_t rows, int64_t k);
+size_t lora_mx4_scales_size(int64_t rows, int64_t k);
+
+/* X [rows, k] (bf16) -> codes and scales, every byte of both written. */
+lora_status lora_mx4_quantize(const lora_bf16* X, uint8_t* codes, uint8_t* scales, int64_t rows, int64_t k,
+                              void* stream);
+
+/* The values that codes and scales stand for, X [rows, k] (bf16, exact). */
+lora_status lora_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, lora_bf16* X, int64_t rows, int64_t k,
+                                void* stream);
+
+/*
+ * Linear layer with a 4-bit weight: Y = Q(X) Q(W)^T, where Q(W) stands in
+ * codes and scales (lora_mx4_quantize of W [n, k], for instance of a merged
+ * weight, lora_linear_merge) and X is quantised on the way.  The products of
+ * 4-bit values and the scales are exact, their sums fp32.
+ *
+ *   X         [m, k] bf16, read only
+ *   W_codes, W_scales   of W [n, k], read only
+ *   Y         [m, n] bf16, written
+ *   workspace at least lora_linear_mx4_fwd_workspace_size(m, n, k) bytes (0 on
+ *             an invalid shape), 16-byte aligned, not used concurrently
+ * A block of X or W with a NaN or an infinity makes every output that it enters
+ * NaN.
+ */
+size_t lora_linear_mx4_fwd_workspace_size(int64_t m, int64_t n, int64_t k);
+lora_status lora_linear_mx4_fwd(const lora_bf16* X, const uint8_t* W_codes, const uint8_t* W_scales, lora_bf16* Y,
+                                void* workspace, size_t workspace_bytes, int64_t m, int64_t n, int64_t k,
+                                void* stream);
+
+/* Type of a row of logits. */
+typedef enum { LORA_BF16 = 0, LORA_F32 = 1 } lora_dtype;
+
+/*
+ * Log probabilities of given tokens under softmax(z / temperature), with the
+ * distribution's entropy and its most probable alternatives:
+ *
+ *     logp[i] = log softmax(z_i / temperature)[tokens[i]]
+ *     entropy[i] = - sum_j softmax(z_i / temperature)[j] log softmax(z_i / temperature)[j]
+ *
+ *   logits   [rows, vocab] of type `dtype` (another: LORA_ERR_UNSUPPORTED), row
+ *            i at element i ld, ld >= vocab (any), read only
+ *   tokens   [rows], or NULL with logp NULL.  A token outside [0, vocab) is
+ *            none: its logp is 0
+ *   temperature  above 0 and finite (else LORA_ERR_SHAPE)
+ *   logp, entropy  [rows] fp32, written
+ *   top      alternatives per row, 0 .. min(vocab, 128) (above vocab
+ *            LORA_ERR_SHAPE, above 128 LORA_ERR_UNSUPPORTED); 0 leaves top_ids
+ *            and top_logp unused (they may be NULL)
+ *   top_ids, top_logp  [rows, top], written: the columns of the largest logits,
+ *            largest first, of equal ones the lowest column first (0 and -0 are
+ *            equal), and their log probabilities
+ *   workspace  at least lora_token_logprobs_workspace_size(rows, vocab, top)
+ *            bytes (0 on invalid arguments), 16-byte aligned, not used
+ *            concurrently
+ * Columns at -inf have probability 0.  A row of -inf alone has entropy 0, logp
+ * and top_logp -inf and the lowest columns as alternatives.  A row with a NaN
+ * or +inf has NaN for logp (of a token), entropy and top_logp; a NaN ranks with
+ * -inf.  rows <= 2^21, vocab <= 2^20, rows x ld <= 2^34.
+ */
+size_t lora_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int64_t top);
+lora_status lora_token_logprobs(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* tokens,
+                                float temperature, float* logp, float* entropy, int32_t* top_ids, float* top_logp,
+                                void* workspace, size_t workspace_bytes, int64_t rows, int64_t vocab, int64_t top,
+                                void* stream);
+
+/*
+ * Distillation from a teacher's top logits.  Row i of the teacher's lists holds
+ * ids id_k and logits t_k, k < top (for instance the top_ids and top_logp of
+ * lora_token_logprobs: adding a number to a row's t changes nothing).  With p =
+ * softmax(t / T) over the entries whose id lies in [0, vocab), q = softmax(z /
+ * T) over the whole vocabulary, T the temperature and w the soft weight,
+ *
+ *     loss[i] = w T^2 sum_k p_k (log p_k - log q[id_k]) - (1 - w) log softmax(z)[labels[i]]
+ *
+ * and for an upstream gradient dloss
+ *
+ *     dlogits[i][j] = dloss[i] ( w T (q_j sum_k p_k - sum_{k: id_k = j} p_k)
+ *                                + (1 - w) (softmax(z)_j - [j = labels[i]]) ).
+ *
+ *   logits   [rows, vocab] as in lora_token_logprobs, read only
+ *   teacher_ids, teacher_logits  [rows, top], 1 <= top <= 128, read only.  An
+ *            entry with an id outside [0, vocab) is left out (lists shorter
+ *            than top); entries of one id add up
+ *   labels   [rows], or NULL with soft_weight 1.  A label outside [0, vocab) is
+ *            none
+ *   temperature  above 0 and finite; soft_weight in [0, 1] (else LORA_ERR_SHAPE)
+ *   loss     [rows] fp32, written
+ *   saved    [rows, 4] fp32: written by the forward for the backward
+ *   dloss    [rows] fp32, read only
+ *   dlogits  [rows, vocab] of the logits' type and row pitch, written (the
+ *            elements between rows are left alone).  It may be the logits
+ *            themselves; any other overlap is LORA_ERR_ALIAS
+ * A row without entries (or with -inf alone as their logits) has no soft term,
+ * one without a label no hard term.  A row of logits of -inf alone has loss and
+ * gradient 0; columns at -inf have gradient 0 but for listed ones, whose loss
+ * is inf.  NaN and +inf in a row's logits, and NaN in its list, give NaN.
+ * Limits as in lora_token_logprobs.
+ *
+ * lora_distill_fwd: the loss (one pass over the logits), and what
+ * lora_distill_bwd needs for the gradient (another pass).  lora_distill_step:
+ * both in one call, for a dloss known beforehand (a mean over the batch): the
+ * logits are read once.
+ */
+lora_status lora_distill_fwd(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* teacher_ids,
+                             const float* teacher_logits, const int32_t* labels, float temperature, float soft_weight,
+                             float* loss, float* saved, int64_t rows, int64_t vocab, int64_t top, void* stream);
+lora_status lora_distill_bwd(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* teacher_ids,
+                             const float* teacher_logits, const int32_t* labels, float temperature, float soft_weight,
+                             const float* saved, const float* dloss, void* dlogits, int64_t rows, int64_t vocab,
+                             int64_t top, void* stream);
+lora_status lora_distill_step(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* teacher_ids,
+                              const float* teacher_logits, const int32_t* labels, float temperature, float soft_weight,
+                              const float* dloss, float* loss, void* dlogits, int64_t rows, int64_t vocab, int64_t top,
+                              void* stream);
+
+/*
  * Launch plan of a call (host only: no GPU, no HIP call, nothing enqueued).
  * Reports, in launch order, the kernels the entry point named by `op` would
  * launch for these shapes -- the same plan the entry point itself executes --

@@ -20,6 +20,10 @@ __all__ = [
     "lora_linear_merge", "lora_linear_fwd_dropout", "lora_linear_bwd_dropout",
     "lora_linear_group_fwd", "lora_linear_group_bwd", "lora_linear_group_bwd_workspace_size",
     "lora_status_string", "STATUS", "lora_linear_plan", "OPS",
+    "lora_mx4_codes_size", "lora_mx4_scales_size", "lora_mx4_quantize", "lora_mx4_dequantize",
+    "lora_linear_mx4_fwd", "lora_linear_mx4_fwd_workspace_size",
+    "lora_token_logprobs", "lora_token_logprobs_workspace_size",
+    "lora_distill_fwd", "lora_distill_bwd", "lora_distill_step",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -88,6 +92,19 @@ def load_library() -> ctypes.CDLL:
     lib.lora_linear_group_bwd_workspace_size.restype = sz
     lib.lora_linear_group_bwd.argtypes = [pa, p, i64, pn, pa, pa, pa, pa, p, pa, pa, p, sz, i64, i64, i64, f32, p]
     lib.lora_linear_group_bwd.restype = ctypes.c_int
+    i32 = ctypes.c_int
+    for name, args, res in (
+            ("lora_mx4_codes_size", [i64, i64], sz), ("lora_mx4_scales_size", [i64, i64], sz),
+            ("lora_mx4_quantize", [p, p, p, i64, i64, p], i32), ("lora_mx4_dequantize", [p, p, p, i64, i64, p], i32),
+            ("lora_linear_mx4_fwd_workspace_size", [i64, i64, i64], sz),
+            ("lora_linear_mx4_fwd", [p, p, p, p, p, sz, i64, i64, i64, p], i32),
+            ("lora_token_logprobs_workspace_size", [i64, i64, i64], sz),
+            ("lora_token_logprobs", [p, i32, i64, p, f32, p, p, p, p, p, sz, i64, i64, i64, p], i32),
+            ("lora_distill_fwd", [p, i32, i64, p, p, p, f32, f32, p, p, i64, i64, i64, p], i32),
+            ("lora_distill_bwd", [p, i32, i64, p, p, p, f32, f32, p, p, p, i64, i64, i64, p], i32),
+            ("lora_distill_step", [p, i32, i64, p, p, p, f32, f32, p, p, p, i64, i64, i64, p], i32)):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, res
     lib.lora_linear_plan.argtypes = [ctypes.c_int, i64, pn, i64, i64, i64, ctypes.POINTER(_LaunchInfo), i64]
     lib.lora_linear_plan.restype = i64
     lib.lora_status_string.argtypes = [ctypes.c_int]
@@ -108,14 +125,14 @@ def _ptr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
-# torch.bfloat16, torch.float32 and the current stream's handle as a call (a
+# torch's types and the current stream's handle as a call (a
 # torch.cuda.Stream object per call costs a microsecond), looked up on the
 # first call that needs them: the host-only functions do without torch.
-_BF16 = _F32 = _current_stream = None
+_BF16 = _F32 = _I32 = _U8 = _current_stream = None
 
 
 def _bind_torch() -> None:
-    global _BF16, _F32, _current_stream
+    global _BF16, _F32, _I32, _U8, _current_stream
     import torch
     raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
     if raw is not None and device is not None:
@@ -123,6 +140,8 @@ def _bind_torch() -> None:
     else:
         _current_stream = lambda: torch.cuda.current_stream().cuda_stream
     _F32 = torch.float32
+    _I32 = torch.int32
+    _U8 = torch.uint8
     _BF16 = torch.bfloat16
 
 
@@ -379,6 +398,191 @@ def lora_linear_group_bwd(dYs, X, Ws, As, Bs, Us, dX, dAs, dBs, workspace, alpha
                                               m, k, r, float(alpha), _stream_handle(stream))
     if st != 0:
         raise LoraError(st, "lora_linear_group_bwd")
+
+
+def lora_mx4_codes_size(rows: int, k: int) -> int:
+    return int(load_library().lora_mx4_codes_size(rows, k))
+
+
+def lora_mx4_scales_size(rows: int, k: int) -> int:
+    return int(load_library().lora_mx4_scales_size(rows, k))
+
+
+def _check_mx4(codes, scales, rows, k, name=""):
+    """4-bit codes [rows, 128 ceil(k/256)] and their scales (any shape of that many bytes)."""
+    if _BF16 is None:
+        _bind_torch()
+    width = (k + 255) // 256
+    if not _fits(codes, _U8, (rows, 128 * width)):
+        _check(codes, name + "codes", _U8, (rows, 128 * width))
+    if scales.numel() != (rows + 63) // 64 * width * 512 or not _fits(scales, _U8, scales.shape):
+        _check(scales, name + "scales", _U8, ((rows + 63) // 64 * width * 512,))
+
+
+def lora_mx4_quantize(X, codes, scales, stream=None) -> None:
+    """X [rows,k] (torch.bfloat16) in microscaled 4 bits: codes [rows, 128 ceil(k/256)]
+    and scales (lora_mx4_scales_size(rows, k) bytes), torch.uint8 (layout in
+    include/lora_linear.h)."""
+    if _BF16 is None:
+        _bind_torch()
+    rows, k = X.shape
+    if not _fits(X, _BF16, (rows, k)):
+        _check(X, "X", _BF16, (rows, k))
+    _check_mx4(codes, scales, rows, k)
+    st = load_library().lora_mx4_quantize(_ptr(X), _ptr(codes), _ptr(scales), rows, k, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_mx4_quantize")
+
+
+def lora_mx4_dequantize(codes, scales, X, stream=None) -> None:
+    """The values that codes and scales stand for, into X [rows,k] (torch.bfloat16)."""
+    if _BF16 is None:
+        _bind_torch()
+    rows, k = X.shape
+    if not _fits(X, _BF16, (rows, k)):
+        _check(X, "X", _BF16, (rows, k))
+    _check_mx4(codes, scales, rows, k)
+    st = load_library().lora_mx4_dequantize(_ptr(codes), _ptr(scales), _ptr(X), rows, k, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_mx4_dequantize")
+
+
+def lora_linear_mx4_fwd_workspace_size(m: int, n: int, k: int) -> int:
+    return int(load_library().lora_linear_mx4_fwd_workspace_size(m, n, k))
+
+
+def lora_linear_mx4_fwd(X, W_codes, W_scales, Y, workspace, stream=None) -> None:
+    """Y = Q(X) Q(W)^T with W [n,k] in microscaled 4 bits and X quantised on the way.
+
+    X [m,k], Y [m,n]: torch.bfloat16; W_codes, W_scales as lora_mx4_quantize
+    writes them; workspace: a device tensor of at least
+    lora_linear_mx4_fwd_workspace_size(m, n, k) bytes."""
+    if _BF16 is None:
+        _bind_torch()
+    m, k = X.shape
+    n = W_codes.shape[0]
+    if not (_fits(X, _BF16, (m, k)) and _fits(Y, _BF16, (m, n))):
+        _check(X, "X", _BF16, (m, k))
+        _check(Y, "Y", _BF16, (m, n))
+    _check_mx4(W_codes, W_scales, n, k, "W_")
+    ws_bytes = _workspace_bytes(workspace)
+    st = load_library().lora_linear_mx4_fwd(_ptr(X), _ptr(W_codes), _ptr(W_scales), _ptr(Y), _ptr(workspace), ws_bytes,
+                                            m, n, k, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_linear_mx4_fwd")
+
+
+def _check_logits(z, name="logits"):
+    """Rows of bf16 or fp32 values of any pitch; returns the type's code, the pitch, rows and columns."""
+    if _BF16 is None:
+        _bind_torch()
+    if z.dtype is not _BF16 and z.dtype is not _F32:
+        raise TypeError(f"{name}: expected torch.bfloat16 or torch.float32, got {z.dtype}")
+    if z.dim() != 2 or not z.is_cuda:
+        raise ValueError(f"{name}: must be a device tensor [rows, vocab]")
+    rows, vocab = z.shape
+    ld, step = z.stride()
+    if (step != 1 and vocab > 1) or (rows > 1 and ld < vocab):
+        raise ValueError(f"{name}: rows must be contiguous and apart from each other")
+    return (1 if z.dtype is _F32 else 0), (ld if rows > 1 else vocab), rows, vocab
+
+
+def _check_rows(*items):
+    for t, name, dtype, shape in items:
+        if not _fits(t, dtype, shape):
+            _check(t, name, dtype, shape)
+
+
+def lora_token_logprobs_workspace_size(rows: int, vocab: int, top: int) -> int:
+    return int(load_library().lora_token_logprobs_workspace_size(rows, vocab, top))
+
+
+def lora_token_logprobs(logits, tokens, logp, entropy, top_ids, top_logp, workspace, temperature: float = 1.0,
+                        stream=None) -> None:
+    """Log probability of each row's token under softmax(logits / temperature), the
+    entropy, and the most probable columns (see include/lora_linear.h).
+
+    logits [rows,vocab]: torch.bfloat16 or torch.float32, rows contiguous, of any
+    pitch; tokens [rows]: torch.int32, or None with logp None; logp, entropy
+    [rows]: torch.float32; top_ids [rows,top]: torch.int32 and top_logp
+    [rows,top]: torch.float32, or both None for no alternatives; workspace: a
+    device tensor of at least lora_token_logprobs_workspace_size(rows, vocab,
+    top) bytes."""
+    code, ld, rows, vocab = _check_logits(logits)
+    if (tokens is None) != (logp is None) or (top_ids is None) != (top_logp is None):
+        raise ValueError("tokens and logp, top_ids and top_logp: both or neither")
+    top = 0 if top_ids is None else top_ids.shape[1]
+    _check_rows((entropy, "entropy", _F32, (rows,)))
+    if tokens is not None:
+        _check_rows((tokens, "tokens", _I32, (rows,)), (logp, "logp", _F32, (rows,)))
+    if top_ids is not None:
+        _check_rows((top_ids, "top_ids", _I32, (rows, top)), (top_logp, "top_logp", _F32, (rows, top)))
+    ws_bytes = _workspace_bytes(workspace)
+    st = load_library().lora_token_logprobs(_ptr(logits), code, ld, _ptr(tokens), float(temperature), _ptr(logp),
+                                            _ptr(entropy), _ptr(top_ids), _ptr(top_logp), _ptr(workspace), ws_bytes,
+                                            rows, vocab, top, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_token_logprobs")
+
+
+def _check_distill(logits, teacher_ids, teacher_logits, labels):
+    code, ld, rows, vocab = _check_logits(logits)
+    top = teacher_ids.shape[1] if teacher_ids.dim() == 2 else 0
+    _check_rows((teacher_ids, "teacher_ids", _I32, (rows, top)), (teacher_logits, "teacher_logits", _F32, (rows, top)))
+    if labels is not None:
+        _check_rows((labels, "labels", _I32, (rows,)))
+    return code, ld, rows, vocab, top
+
+
+def _check_dlogits(dlogits, logits, ld):
+    code, ldd, rows, vocab = _check_logits(dlogits, "dlogits")
+    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape or ldd != ld:
+        raise ValueError("dlogits: must be of the logits' type, shape and row pitch")
+
+
+def lora_distill_fwd(logits, teacher_ids, teacher_logits, labels, loss, saved, temperature: float = 1.0,
+                     soft_weight: float = 1.0, stream=None) -> None:
+    """Loss of every row of distillation from a teacher's top logits (see
+    include/lora_linear.h), and what lora_distill_bwd needs in `saved`.
+
+    logits as in lora_token_logprobs; teacher_ids [rows,top]: torch.int32 (-1: no
+    entry); teacher_logits [rows,top]: torch.float32; labels [rows]: torch.int32,
+    or None with soft_weight 1; loss [rows], saved [rows,4]: torch.float32."""
+    code, ld, rows, vocab, top = _check_distill(logits, teacher_ids, teacher_logits, labels)
+    _check_rows((loss, "loss", _F32, (rows,)), (saved, "saved", _F32, (rows, 4)))
+    st = load_library().lora_distill_fwd(_ptr(logits), code, ld, _ptr(teacher_ids), _ptr(teacher_logits), _ptr(labels),
+                                         float(temperature), float(soft_weight), _ptr(loss), _ptr(saved), rows, vocab,
+                                         top, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_distill_fwd")
+
+
+def lora_distill_bwd(logits, teacher_ids, teacher_logits, labels, saved, dloss, dlogits, temperature: float = 1.0,
+                     soft_weight: float = 1.0, stream=None) -> None:
+    """Gradient of lora_distill_fwd's loss for an upstream dloss [rows]
+    (torch.float32), into dlogits of the logits' type, shape and row pitch (it may
+    be the logits tensor itself)."""
+    code, ld, rows, vocab, top = _check_distill(logits, teacher_ids, teacher_logits, labels)
+    _check_rows((saved, "saved", _F32, (rows, 4)), (dloss, "dloss", _F32, (rows,)))
+    _check_dlogits(dlogits, logits, ld)
+    st = load_library().lora_distill_bwd(_ptr(logits), code, ld, _ptr(teacher_ids), _ptr(teacher_logits), _ptr(labels),
+                                         float(temperature), float(soft_weight), _ptr(saved), _ptr(dloss),
+                                         _ptr(dlogits), rows, vocab, top, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_distill_bwd")
+
+
+def lora_distill_step(logits, teacher_ids, teacher_logits, labels, dloss, loss, dlogits, temperature: float = 1.0,
+                      soft_weight: float = 1.0, stream=None) -> None:
+    """lora_distill_fwd and lora_distill_bwd in one call that reads the logits once."""
+    code, ld, rows, vocab, top = _check_distill(logits, teacher_ids, teacher_logits, labels)
+    _check_rows((loss, "loss", _F32, (rows,)), (dloss, "dloss", _F32, (rows,)))
+    _check_dlogits(dlogits, logits, ld)
+    st = load_library().lora_distill_step(_ptr(logits), code, ld, _ptr(teacher_ids), _ptr(teacher_logits), _ptr(labels),
+                                          float(temperature), float(soft_weight), _ptr(dloss), _ptr(loss),
+                                          _ptr(dlogits), rows, vocab, top, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_distill_step")
 
 
 def lora_linear_plan(op: str, m: int, n, k: int, r: int) -> list:

@@ -1,0 +1,198 @@
+// Microscaled 4-bit matrices: quantisation, its inverse, and the linear layer
+// Y = Q(X) Q(W)^T on the matrix cores' scaled 4-bit products.
+//
+// v_mfma_scale_f32_16x16x128_f8f6f4 takes 16 rows of A and 16 of B over 128 k
+// in 4 bits and a scale byte per row and 32 k.  With c = l % 16, g = l / 16,
+// lane l holds row c, k = 32 g .. + 31 (16 bytes), and that block's scale; the
+// result holds column c (B's row), rows 4 g .. 4 g + 3 (A's).  A row of 64 bytes
+// so feeds the same product time as 32 bf16 k, and the operands of a 256-column
+// slab (128 bytes a row) take two products.
+#include <type_traits>
+
+#include "lora_device.hpp"
+#include "lora_ops.hpp"
+#include "lora_plan.hpp"
+
+namespace lora {
+
+typedef int int8v __attribute__((ext_vector_type(8)));
+
+// acc += A B^T over one 128-wide step; SA and SB pick the scale byte of sa and sb.
+template <int SA, int SB>
+__device__ __forceinline__ floatx4 mfma_mx4(int4v a, int4v b, floatx4 acc, int sa, int sb) {
+  const int8v A{a[0], a[1], a[2], a[3], 0, 0, 0, 0}, B{b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc, 4, 4, SA, sa, SB, sb);
+}
+
+// Scale byte of a row's block within its cell; bytes of 32-row-block b of
+// four rows 16 apart follow each other.
+__device__ __forceinline__ int mx4_scale_offset(int row, int block) {
+  return (block & 3) * 128 + (row & 15) * 8 + ((row >> 4) & 3) * 2 + ((block >> 2) & 1);
+}
+
+// ---------------------------------------------------------------------------
+// Quantisation.  A workgroup takes a cell of scales, 64 rows x 256 columns: four
+// lanes a block, each 8 columns.  Reads 2 bytes and writes 0.53 a column; bound
+// by HBM.
+__global__ __launch_bounds__(256) void lora_mx4_quantize_kernel(const u16* __restrict__ X, uint8_t* __restrict__ codes,
+                                                                uint8_t* __restrict__ scales, int rows, int k,
+                                                                int slabs, int groups) {
+  __shared__ __attribute__((aligned(16))) uint8_t cell[512];
+  const int slab = (int)blockIdx.x % slabs, grp = (int)blockIdx.x / slabs;
+  const int tid = threadIdx.x, piece = tid & 31, col = slab * 256 + 8 * piece;
+  const bool inside = col < k;
+  int4v x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = grp * 64 + (tid >> 5) + 8 * i;
+    x[i] = inside && row < rows ? *reinterpret_cast<const int4v*>(X + (size_t)row * k + col) : int4v{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int lrow = (tid >> 5) + 8 * i, row = grp * 64 + lrow;
+    uint32_t top = 0;   // the largest magnitude's bits
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const uint32_t w = (uint32_t)x[i][h] & 0x7FFF7FFFu;
+      top = max(top, max(w & 0xFFFFu, w >> 16));
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    const int field = (int)(top >> 7);
+    const bool nan = field == 255;
+    const int scale = nan ? 255 : max(field - 2, 0);
+    // x 2^(127 - scale) is exact; the conversion rounds to nearest even and saturates
+    const float up = __builtin_bit_cast(float, (uint32_t)(254 - scale) << 23);
+    uint32_t out = 0;
+    if (!nan) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = bf16_to_f32((u16)((uint32_t)x[i][e >> 1] >> (16 * (e & 1)))) * up;
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, y[0], y[1], 1.0f, 0);
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, y[2], y[3], 1.0f, 1);
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, y[4], y[5], 1.0f, 2);
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(out, y[6], y[7], 1.0f, 3);
+    }
+    const int block = slab * 8 + (piece >> 2);
+    if ((piece & 3) == 0) cell[mx4_scale_offset(lrow, block)] = (uint8_t)(row < rows && block * 32 < k ? scale : 0);
+    if (row < rows) *reinterpret_cast<uint32_t*>(codes + ((size_t)row * slabs + slab) * 128 + piece * 4) = out;
+  }
+  __syncthreads();
+  if (tid < 32)
+    reinterpret_cast<int4v*>(scales + ((size_t)slab * groups + grp) * 512)[tid] = reinterpret_cast<const int4v*>(cell)[tid];
+}
+
+// The values of codes and scales: a lane takes 8 columns.
+__global__ __launch_bounds__(256) void lora_mx4_dequantize_kernel(const uint8_t* __restrict__ codes,
+                                                                  const uint8_t* __restrict__ scales,
+                                                                  u16* __restrict__ X, int rows, int k, int slabs,
+                                                                  int groups) {
+  const int slab = (int)blockIdx.x % slabs, grp = (int)blockIdx.x / slabs;
+  const int tid = threadIdx.x, piece = tid & 31, col = slab * 256 + 8 * piece, block = slab * 8 + (piece >> 2);
+  if (col >= k) return;
+  const uint8_t* cell = scales + ((size_t)slab * groups + grp) * 512;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int lrow = (tid >> 5) + 8 * i, row = grp * 64 + lrow;
+    if (row >= rows) continue;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + ((size_t)row * slabs + slab) * 128 + piece * 4);
+    const int s = cell[mx4_scale_offset(lrow, block)];
+    // 2^(s - 127); s = 0 is a subnormal, 255 NaN
+    const uint32_t bits = s == 0 ? 0x00400000u : (s == 255 ? 0x7FC00000u : (uint32_t)s << 23);
+    const float unit = __builtin_bit_cast(float, bits);
+    const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+    const auto p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+    const float y[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+    int4v o;
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      o[h] = (int)((uint32_t)f32_to_bf16(y[2 * h] * unit) | ((uint32_t)f32_to_bf16(y[2 * h + 1] * unit) << 16));
+    *reinterpret_cast<int4v*>(X + (size_t)row * k + col) = o;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Y = Q(X) Q(W)^T straight from memory: a workgroup forms 16 features x 16 TG
+// tokens, its four waves taking the slabs in turn; their sums are added in wave
+// order through LDS.
+template <int TG>
+__global__ __launch_bounds__(256) void lora_mx4_direct_kernel(const uint8_t* __restrict__ Xc,
+                                                              const uint8_t* __restrict__ Xs,
+                                                              const uint8_t* __restrict__ Wc,
+                                                              const uint8_t* __restrict__ Ws, u16* __restrict__ Y, int m,
+                                                              int n, int slabs, int tiles_n) {
+  __shared__ floatx4 part[4][TG][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int g = lane >> 4, c = lane & 15;
+  const int n0 = (int)(blockIdx.x % (unsigned)tiles_n) * 16, m0 = (int)(blockIdx.x / (unsigned)tiles_n) * 16 * TG;
+  const int gw = (n + 63) / 64, gx = (m + 63) / 64;
+  const int wrow = min(n0 + c, n - 1);
+  const uint8_t* wp = Wc + (size_t)wrow * slabs * 128 + 16 * g;
+  const uint8_t* wsp = Ws + (size_t)(wrow >> 6) * 512 + mx4_scale_offset(wrow, g);
+  const uint8_t *xp[TG], *xsp[TG];
+#pragma unroll
+  for (int t = 0; t < TG; ++t) {
+    const int row = min(m0 + 16 * t + c, m - 1);
+    xp[t] = Xc + (size_t)row * slabs * 128 + 16 * g;
+    xsp[t] = Xs + (size_t)(row >> 6) * 512 + mx4_scale_offset(row, g);
+  }
+  floatx4 acc[TG];
+#pragma unroll
+  for (int t = 0; t < TG; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int s = wave; s < slabs; s += 4) {
+    const int4v w0 = *reinterpret_cast<const int4v*>(wp + (size_t)s * 128);
+    const int4v w1 = *reinterpret_cast<const int4v*>(wp + (size_t)s * 128 + 64);
+    const int ws = *reinterpret_cast<const u16*>(wsp + (size_t)s * gw * 512);
+#pragma unroll
+    for (int t = 0; t < TG; ++t) {
+      const int4v x0 = *reinterpret_cast<const int4v*>(xp[t] + (size_t)s * 128);
+      const int4v x1 = *reinterpret_cast<const int4v*>(xp[t] + (size_t)s * 128 + 64);
+      const int xs = *reinterpret_cast<const u16*>(xsp[t] + (size_t)s * gx * 512);
+      acc[t] = mfma_mx4<0, 0>(w0, x0, acc[t], ws, xs);
+      acc[t] = mfma_mx4<1, 1>(w1, x1, acc[t], ws, xs);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < TG; ++t) part[wave][t][lane] = acc[t];
+  __syncthreads();
+  for (int t = wave; t < TG; t += 4) {
+    const floatx4 v = ((part[0][t][lane] + part[1][t][lane]) + part[2][t][lane]) + part[3][t][lane];
+    const int row = m0 + 16 * t + c, col = n0 + 4 * g;
+    if (row < m && col < n) {
+      const uint32_t lo = (uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16);
+      const uint32_t hi = (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16);
+      *reinterpret_cast<uint2*>(Y + (size_t)row * n + col) = uint2{lo, hi};
+    }
+  }
+}
+
+hipError_t launch_mx4_quantize(const Mx4QuantArgs& a, hipStream_t st) {
+  const int slabs = (int)mx4_slabs(a.k), groups = (int)mx4_groups(a.rows);
+  hipLaunchKernelGGL(lora_mx4_quantize_kernel, dim3((unsigned)(slabs * groups)), dim3(256), 0, st, a.X, a.codes, a.scales,
+                     (int)a.rows, (int)a.k, slabs, groups);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, uint16_t* X, int64_t rows, int64_t k,
+                                 hipStream_t st) {
+  const int slabs = (int)mx4_slabs(k), groups = (int)mx4_groups(rows);
+  hipLaunchKernelGGL(lora_mx4_dequantize_kernel, dim3((unsigned)(slabs * groups)), dim3(256), 0, st, codes, scales, X,
+                     (int)rows, (int)k, slabs, groups);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_fwd(const Mx4FwdArgs& a, hipStream_t st) {
+  const Mx4Layout L = mx4_fwd_layout(a.m, a.n, a.k);
+  uint8_t* xc = reinterpret_cast<uint8_t*>(a.ws + L.xc);
+  uint8_t* xs = reinterpret_cast<uint8_t*>(a.ws + L.xs);
+  const hipError_t e = launch_mx4_quantize(Mx4QuantArgs{a.X, xc, xs, a.m, a.k}, st);
+  if (e != hipSuccess) return e;
+  constexpr int TG = 4;
+  const int tiles_n = (int)((a.n + 15) / 16);
+  const int64_t tiles_m = (a.m + 16 * TG - 1) / (16 * TG);
+  hipLaunchKernelGGL((lora_mx4_direct_kernel<TG>), dim3((unsigned)(tiles_m * tiles_n)), dim3(256), 0, st, xc, xs, a.Wc,
+                     a.Ws, a.Y, (int)a.m, (int)a.n, (int)mx4_slabs(a.k), tiles_n);
+  return hipGetLastError();
+}
+
+}  // namespace lora
