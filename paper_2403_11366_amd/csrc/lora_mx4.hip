@@ -166,6 +166,204 @@ __global__ __launch_bounds__(256) void lora_mx4_direct_kernel(const uint8_t* __r
   }
 }
 
+// ---------------------------------------------------------------------------
+// 256 x 256 tiles: eight waves of 128 tokens x 64 features, two slabs in LDS,
+// copied from memory straight into LDS (one 16-byte chunk a lane, the swizzle
+// applied to the global addresses).
+//
+// The two wave rows take turns: waves w and w + 4 share a SIMD, and while one
+// multiplies, the other reads its next fragments and issues copies; a workgroup
+// barrier ends each slot and the second row runs one slot behind.  A slab is
+// four phases, each a slot of reads and a slot of sixteen products: (W half 0, X
+// half 0), (W 1, X 0), (W 0, X 1), (W 1, X 1), reading X half 0, W half 1, X half
+// 1 and the next slab's W half 0.  Every wave waits for its reads before the
+// barrier that ends its read slot, so the quarter read in phase P is free from
+// the read slots of phase P + 1 on, which refill it for the slab after next.
+// The quarter read in phase P + 1 is waited for in the read slot of P, with six
+// newer quarters (two copies each) in flight.
+//
+// The scales go straight to registers, three 8-byte loads a wave and slab (64 of
+// its tokens, the other 64, its features), issued at the start of the slab
+// before, ahead of that slab's copies: at any wait at least three of them are
+// newer than the quarter waited for.
+template <typename F, int... I>
+__device__ __forceinline__ void each_const(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F&& f) {
+  each_const(std::make_integer_sequence<int, N>{}, f);
+}
+
+__global__ __launch_bounds__(512) void lora_mx4_big_kernel(const uint8_t* __restrict__ Xc,
+                                                           const uint8_t* __restrict__ Xs,
+                                                           const uint8_t* __restrict__ Wc,
+                                                           const uint8_t* __restrict__ Ws, u16* __restrict__ Y, int m,
+                                                           int n, int slabs, int tiles_m, int tiles_n) {
+  constexpr int BM = 256, BN = 256, STAGE = (BM + BN) * 128;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  int tm, tn;
+  tile_coords(tiles_m, tiles_n, 8, (int)blockIdx.x, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const int g = lane >> 4, c16 = lane & 15;
+
+  const uint32_t rowbytes = (uint32_t)slabs * 128;
+  const __amdgpu_buffer_rsrc_t rsX = make_rsrc(Xc + (size_t)m0 * rowbytes, (uint64_t)min(BM, m - m0) * rowbytes);
+  const __amdgpu_buffer_rsrc_t rsW = make_rsrc(Wc + (size_t)n0 * rowbytes, (uint64_t)min(BN, n - n0) * rowbytes);
+  // scales from the wave's first cell on (cells past the matrix: another's, or zeros past the end)
+  const int gx = (m + 63) / 64, gw = (n + 63) / 64, cx = m0 / 64 + 2 * wm, cw = n0 / 64 + wn;
+  const __amdgpu_buffer_rsrc_t rsXs = make_rsrc(Xs, (uint64_t)gx * slabs * 512);
+  const __amdgpu_buffer_rsrc_t rsWs = make_rsrc(Ws, (uint64_t)gw * slabs * 512);
+  const uint32_t cell = (uint32_t)(g * 128 + c16 * 8);
+
+  floatx4 acc[4][8];           // 16 x 16 fragments: [features 16 a ..][tokens 16 b ..] of the wave's 64 x 128
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int b = 0; b < 8; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+  int4v fw[2][2][2], fx[2][4];   // W halves [half][step][fragment], the current X half [step][fragment]
+  uint2 sx[2], sw, sx1[2], sw1;  // scales of this slab (two token cells, the feature cell) and the next
+
+  const int l8 = lane >> 3;
+  const int xrow = 8 * wave, wrow = 64 * (wave >> 2) + 8 * (wave & 3);
+  const uint32_t kcol = (uint32_t)(((lane & 7) ^ kc_swz(xrow + l8)) << 4);
+  const uint32_t xoff = (uint32_t)(xrow + l8) * rowbytes + kcol;
+  const uint32_t woff = (uint32_t)(wrow + l8) * rowbytes + kcol;
+  auto copy_x = [&](int kb, int h) LORA_INLINE {
+    char* sb = smem + (kb & 1) * STAGE + xrow * 128 + h * 8192;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      dma16(rsX, xoff + (uint32_t)(64 * h + 128 * i) * rowbytes, (uint32_t)kb * 128, sb + i * 16384);
+  };
+  auto copy_w = [&](int kb, int h) LORA_INLINE {
+    char* sb = smem + (kb & 1) * STAGE + BM * 128 + wrow * 128 + h * 4096;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      dma16(rsW, woff + (uint32_t)(32 * h + 128 * i) * rowbytes, (uint32_t)kb * 128, sb + i * 16384);
+  };
+  auto load_scales = [&](int kb) LORA_INLINE {   // three loads, in this place
+    __builtin_amdgcn_sched_barrier(0);
+    sx1[0] = buf_load8(rsXs, ((uint32_t)kb * gx + cx) * 512 + cell);
+    sx1[1] = buf_load8(rsXs, ((uint32_t)kb * gx + cx + 1) * 512 + cell);
+    sw1 = buf_load8(rsWs, ((uint32_t)kb * gw + cw) * 512 + cell);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto next_scales = [&]() LORA_INLINE {
+    sx[0] = sx1[0];
+    sx[1] = sx1[1];
+    sw = sw1;
+  };
+  auto read_x = [&](int kb, int h) LORA_INLINE {
+    const char* xs = smem + (kb & 1) * STAGE;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        fx[kk][b] = *reinterpret_cast<const int4v*>(xs + kc_offset(wm * 128 + 64 * h + 16 * b + c16, 4 * kk + g));
+  };
+  auto read_w = [&](int kb, int h) LORA_INLINE {
+    const char* ws = smem + (kb & 1) * STAGE + BM * 128;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+        fw[h][kk][a] = *reinterpret_cast<const int4v*>(ws + kc_offset(wn * 64 + 32 * h + 16 * a + c16, 4 * kk + g));
+  };
+  auto slot_end = [&]() LORA_INLINE {
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto products = [&](auto hwc, auto hxc) LORA_INLINE {
+    constexpr int HW = decltype(hwc)::value, HX = decltype(hxc)::value;
+    const int sa = (int)(HW ? sw.y : sw.x);
+    unrolled<16>([&](auto ic) LORA_INLINE {
+      constexpr int I = decltype(ic)::value, KK = I >> 3, A = (I >> 2) & 1, B = I & 3;
+      const int sb = (int)(B >> 1 ? sx[HX].y : sx[HX].x);
+      acc[2 * HW + A][4 * HX + B] = mfma_mx4<2 * A + KK, 2 * (B & 1) + KK>(fw[HW][KK][A], fx[KK][B],
+                                                                         acc[2 * HW + A][4 * HX + B], sa, sb);
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    slot_end();
+  };
+  auto ready = [&](auto left) LORA_INLINE {   // reads done; at most `left` quarters' copies and three scales in flight
+    constexpr int L = decltype(left)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    wait_lgkm0();
+    wait_vmcnt<L ? 2 * L + 3 : 0>();
+    slot_end();
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  using I3 = std::integral_constant<int, 3>;
+  using I4 = std::integral_constant<int, 4>;
+  using I5 = std::integral_constant<int, 5>;
+  using I6 = std::integral_constant<int, 6>;
+  auto stage = [&](int kb, auto mode) LORA_INLINE {   // 0: steady, 1: the last but one, 2: the last
+    constexpr int MODE = decltype(mode)::value;
+    next_scales();
+    if constexpr (MODE < 2) load_scales(kb + 1);
+    read_x(kb, 0);
+    if constexpr (MODE == 0) { copy_w(kb + 2, 0); ready(I6{}); }
+    else if constexpr (MODE == 1) ready(I5{});
+    else ready(I1{});
+    products(I0{}, I0{});
+    read_w(kb, 1);
+    if constexpr (MODE == 0) { copy_x(kb + 2, 0); ready(I6{}); }
+    else if constexpr (MODE == 1) ready(I4{});
+    else ready(I0{});
+    products(I1{}, I0{});
+    read_x(kb, 1);
+    if constexpr (MODE == 0) { copy_w(kb + 2, 1); ready(I6{}); }
+    else if constexpr (MODE == 1) ready(I3{});
+    else ready(I0{});
+    products(I0{}, I1{});
+    if constexpr (MODE < 2) read_w(kb + 1, 0);
+    if constexpr (MODE == 0) { copy_x(kb + 2, 1); ready(I6{}); }
+    else if constexpr (MODE == 1) ready(I2{});
+    else ready(I0{});
+    products(I1{}, I1{});
+  };
+  load_scales(0);
+  copy_w(0, 0); copy_x(0, 0); copy_w(0, 1); copy_x(0, 1);
+  if (slabs > 1) {
+    copy_w(1, 0); copy_x(1, 0); copy_w(1, 1); copy_x(1, 1);
+    wait_vmcnt<12>();
+  } else {
+    wait_vmcnt<0>();
+  }
+  slot_end();
+  read_w(0, 0);
+  __builtin_amdgcn_sched_barrier(0);
+  wait_lgkm0();
+  slot_end();                    // every wave has read the quarter that the first read slot refills
+  if (wm == 1) slot_end();       // the second wave row runs one slot behind
+  int kb = 0;
+  for (; kb + 2 < slabs; ++kb) stage(kb, I0{});
+  if (slabs > 1) stage(kb++, I1{});
+  stage(kb, I2{});
+  if (wm == 0) slot_end();
+
+  // Y: each wave's blocks of 32 tokens x 64 features through a region of LDS of its own
+  constexpr int OUT = out16_bytes<4, 2>();
+  static_assert(8 * OUT <= 2 * STAGE, "output staging");
+  __syncthreads();
+  const int j0 = n0 + wn * 64;
+#pragma unroll
+  for (int fi = 0; fi < 4; ++fi) {
+    const int i0 = m0 + wm * 128 + 32 * fi;
+    floatx4 v[4][2];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      v[a][0] = acc[a][2 * fi];
+      v[a][1] = acc[a][2 * fi + 1];
+    }
+    store_out16<4, 2>(v, smem + wave * OUT, Y + (size_t)i0 * n + j0, (size_t)n, m - i0, n - j0, lane);
+  }
+}
+
 hipError_t launch_mx4_quantize(const Mx4QuantArgs& a, hipStream_t st) {
   const int slabs = (int)mx4_slabs(a.k), groups = (int)mx4_groups(a.rows);
   hipLaunchKernelGGL(lora_mx4_quantize_kernel, dim3((unsigned)(slabs * groups)), dim3(256), 0, st, a.X, a.codes, a.scales,
@@ -187,6 +385,12 @@ hipError_t launch_mx4_fwd(const Mx4FwdArgs& a, hipStream_t st) {
   uint8_t* xs = reinterpret_cast<uint8_t*>(a.ws + L.xs);
   const hipError_t e = launch_mx4_quantize(Mx4QuantArgs{a.X, xc, xs, a.m, a.k}, st);
   if (e != hipSuccess) return e;
+  if (a.m > 64) {
+    const int tm = (int)((a.m + 255) / 256), tn = (int)((a.n + 255) / 256);
+    hipLaunchKernelGGL(lora_mx4_big_kernel, dim3((unsigned)(tm * tn)), dim3(512), 0, st, xc, xs, a.Wc, a.Ws, a.Y,
+                       (int)a.m, (int)a.n, (int)mx4_slabs(a.k), tm, tn);
+    return hipGetLastError();
+  }
   constexpr int TG = 4;
   const int tiles_n = (int)((a.n + 15) / 16);
   const int64_t tiles_m = (a.m + 16 * TG - 1) / (16 * TG);
