@@ -171,21 +171,17 @@ __global__ __launch_bounds__(256) void lora_mx4_direct_kernel(const uint8_t* __r
 // copied from memory straight into LDS (one 16-byte chunk a lane, the swizzle
 // applied to the global addresses).
 //
-// The two wave rows take turns: waves w and w + 4 share a SIMD, and while one
-// multiplies, the other reads its next fragments and issues copies; a workgroup
-// barrier ends each slot and the second row runs one slot behind.  A slab is
-// four phases, each a slot of reads and a slot of sixteen products: (W half 0, X
-// half 0), (W 1, X 0), (W 0, X 1), (W 1, X 1), reading X half 0, W half 1, X half
-// 1 and the next slab's W half 0.  Every wave waits for its reads before the
-// barrier that ends its read slot, so the quarter read in phase P is free from
-// the read slots of phase P + 1 on, which refill it for the slab after next.
-// The quarter read in phase P + 1 is waited for in the read slot of P, with six
-// newer quarters (two copies each) in flight.
+// A slab is two 128-wide steps.  A wave holds a step's fragments in registers
+// and, as soon as the four products of a token fragment are issued, reads that
+// fragment of the next step into its place; the feature fragments have a second
+// set.  So no wave waits for LDS at a step's start.  The one barrier of a slab
+// stands between its steps: every wave has read the whole slab, whose place the
+// second step fills with the slab after next, and the next slab has landed.
 //
 // The scales go straight to registers, three 8-byte loads a wave and slab (64 of
-// its tokens, the other 64, its features), issued at the start of the slab
-// before, ahead of that slab's copies: at any wait at least three of them are
-// newer than the quarter waited for.
+// its tokens, the other 64, its features), a slab ahead of their use; they are
+// issued after that slab's copies, so three loads may be under way when the
+// copies are waited for.
 template <typename F, int... I>
 __device__ __forceinline__ void each_const(std::integer_sequence<int, I...>, F&& f) {
   (f(std::integral_constant<int, I>{}), ...);
@@ -223,25 +219,17 @@ __global__ __launch_bounds__(512) void lora_mx4_big_kernel(const uint8_t* __rest
   for (int a = 0; a < 4; ++a)
 #pragma unroll
     for (int b = 0; b < 8; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-  int4v fw[2][2][2], fx[2][4];   // W halves [half][step][fragment], the current X half [step][fragment]
+  int4v fw[2][4], fx[8];         // W fragments of both steps, X fragments of the current one
   uint2 sx[2], sw, sx1[2], sw1;  // scales of this slab (two token cells, the feature cell) and the next
 
-  const int l8 = lane >> 3;
-  const int xrow = 8 * wave, wrow = 64 * (wave >> 2) + 8 * (wave & 3);
-  const uint32_t kcol = (uint32_t)(((lane & 7) ^ kc_swz(xrow + l8)) << 4);
-  const uint32_t xoff = (uint32_t)(xrow + l8) * rowbytes + kcol;
-  const uint32_t woff = (uint32_t)(wrow + l8) * rowbytes + kcol;
-  auto copy_x = [&](int kb, int h) LORA_INLINE {
-    char* sb = smem + (kb & 1) * STAGE + xrow * 128 + h * 8192;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      dma16(rsX, xoff + (uint32_t)(64 * h + 128 * i) * rowbytes, (uint32_t)kb * 128, sb + i * 16384);
-  };
-  auto copy_w = [&](int kb, int h) LORA_INLINE {
-    char* sb = smem + (kb & 1) * STAGE + BM * 128 + wrow * 128 + h * 4096;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      dma16(rsW, woff + (uint32_t)(32 * h + 128 * i) * rowbytes, (uint32_t)kb * 128, sb + i * 16384);
+  // a wave copies 8 rows of X and of W per instruction, four of each a slab
+  const int l8 = lane >> 3, crow = 8 * wave;
+  const uint32_t kcol = (uint32_t)(((lane & 7) ^ kc_swz(crow + l8)) << 4);
+  const uint32_t coff = (uint32_t)(crow + l8) * rowbytes + kcol;
+  auto copy = [&](int kb, int i) LORA_INLINE {
+    char* sb = smem + (kb & 1) * STAGE + (crow + 64 * i) * 128;
+    dma16(rsX, coff + (uint32_t)(64 * i) * rowbytes, (uint32_t)kb * 128, sb);
+    dma16(rsW, coff + (uint32_t)(64 * i) * rowbytes, (uint32_t)kb * 128, sb + BM * 128);
   };
   auto load_scales = [&](int kb) LORA_INLINE {   // three loads, in this place
     __builtin_amdgcn_sched_barrier(0);
@@ -250,101 +238,73 @@ __global__ __launch_bounds__(512) void lora_mx4_big_kernel(const uint8_t* __rest
     sw1 = buf_load8(rsWs, ((uint32_t)kb * gw + cw) * 512 + cell);
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto next_scales = [&]() LORA_INLINE {
-    sx[0] = sx1[0];
-    sx[1] = sx1[1];
-    sw = sw1;
+  const uint32_t fbase = kc_offset(c16, g);      // (rows 16 apart swizzle alike; step 1: chunk 4 further)
+  auto read_x = [&](int kb, int step, int b) LORA_INLINE {
+    const char* xs = smem + (kb & 1) * STAGE + wm * 128 * 128;
+    fx[b] = *reinterpret_cast<const int4v*>(xs + (fbase ^ (step << 6)) + 16 * 128 * b);
   };
-  auto read_x = [&](int kb, int h) LORA_INLINE {
-    const char* xs = smem + (kb & 1) * STAGE;
+  auto read_w = [&](int kb, int step) LORA_INLINE {
+    const char* ws = smem + (kb & 1) * STAGE + (BM + wn * 64) * 128;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-        fx[kk][b] = *reinterpret_cast<const int4v*>(xs + kc_offset(wm * 128 + 64 * h + 16 * b + c16, 4 * kk + g));
+    for (int a = 0; a < 4; ++a)
+      fw[step][a] = *reinterpret_cast<const int4v*>(ws + (fbase ^ (step << 6)) + 16 * 128 * a);
   };
-  auto read_w = [&](int kb, int h) LORA_INLINE {
-    const char* ws = smem + (kb & 1) * STAGE + BM * 128;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int a = 0; a < 2; ++a)
-        fw[h][kk][a] = *reinterpret_cast<const int4v*>(ws + kc_offset(wn * 64 + 32 * h + 16 * a + c16, 4 * kk + g));
-  };
-  auto slot_end = [&]() LORA_INLINE {
-    asm volatile("s_barrier" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  auto products = [&](auto hwc, auto hxc) LORA_INLINE {
-    constexpr int HW = decltype(hwc)::value, HX = decltype(hxc)::value;
-    const int sa = (int)(HW ? sw.y : sw.x);
-    unrolled<16>([&](auto ic) LORA_INLINE {
-      constexpr int I = decltype(ic)::value, KK = I >> 3, A = (I >> 2) & 1, B = I & 3;
-      const int sb = (int)(B >> 1 ? sx[HX].y : sx[HX].x);
-      acc[2 * HW + A][4 * HX + B] = mfma_mx4<2 * A + KK, 2 * (B & 1) + KK>(fw[HW][KK][A], fx[KK][B],
-                                                                         acc[2 * HW + A][4 * HX + B], sa, sb);
+  // products of a step; after each token fragment's four, f(its index)
+  auto products = [&](auto stepc, auto&& f) LORA_INLINE {
+    constexpr int S = decltype(stepc)::value;
+    unrolled<8>([&](auto bc) LORA_INLINE {
+      constexpr int B = decltype(bc)::value;
+      const int sb = (int)((B >> 1) & 1 ? sx[B >> 2].y : sx[B >> 2].x);
+      unrolled<4>([&](auto ac) LORA_INLINE {
+        constexpr int A = decltype(ac)::value;
+        const int sa = (int)(A >> 1 ? sw.y : sw.x);
+        acc[A][B] = mfma_mx4<2 * (A & 1) + S, 2 * (B & 1) + S>(fw[S][A], fx[B], acc[A][B], sa, sb);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+      f(B);
+      __builtin_amdgcn_sched_barrier(0);
     });
-    __builtin_amdgcn_sched_barrier(0);
-    slot_end();
-  };
-  auto ready = [&](auto left) LORA_INLINE {   // reads done; at most `left` quarters' copies and three scales in flight
-    constexpr int L = decltype(left)::value;
-    __builtin_amdgcn_sched_barrier(0);
-    wait_lgkm0();
-    wait_vmcnt<L ? 2 * L + 3 : 0>();
-    slot_end();
   };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
   using I2 = std::integral_constant<int, 2>;
-  using I3 = std::integral_constant<int, 3>;
-  using I4 = std::integral_constant<int, 4>;
-  using I5 = std::integral_constant<int, 5>;
-  using I6 = std::integral_constant<int, 6>;
-  auto stage = [&](int kb, auto mode) LORA_INLINE {   // 0: steady, 1: the last but one, 2: the last
+  auto slab = [&](int kb, auto mode) LORA_INLINE {   // 0: steady, 1: the last but one, 2: the last
     constexpr int MODE = decltype(mode)::value;
-    next_scales();
+    sx[0] = sx1[0];
+    sx[1] = sx1[1];
+    sw = sw1;
     if constexpr (MODE < 2) load_scales(kb + 1);
-    read_x(kb, 0);
-    if constexpr (MODE == 0) { copy_w(kb + 2, 0); ready(I6{}); }
-    else if constexpr (MODE == 1) ready(I5{});
-    else ready(I1{});
-    products(I0{}, I0{});
-    read_w(kb, 1);
-    if constexpr (MODE == 0) { copy_x(kb + 2, 0); ready(I6{}); }
-    else if constexpr (MODE == 1) ready(I4{});
-    else ready(I0{});
-    products(I1{}, I0{});
-    read_x(kb, 1);
-    if constexpr (MODE == 0) { copy_w(kb + 2, 1); ready(I6{}); }
-    else if constexpr (MODE == 1) ready(I3{});
-    else ready(I0{});
-    products(I0{}, I1{});
-    if constexpr (MODE < 2) read_w(kb + 1, 0);
-    if constexpr (MODE == 0) { copy_x(kb + 2, 1); ready(I6{}); }
-    else if constexpr (MODE == 1) ready(I2{});
-    else ready(I0{});
-    products(I1{}, I1{});
+    products(I0{}, [&](int b) LORA_INLINE {
+      if (b == 1) read_w(kb, 1);
+      read_x(kb, 1, b);
+    });
+    if constexpr (MODE < 2) {
+      copy_barrier<3>();   // every wave has read this slab, and the next one has landed
+      read_w(kb + 1, 0);
+    }
+    products(I1{}, [&](int b) LORA_INLINE {
+      if constexpr (MODE == 0)
+        if (b < 4) copy(kb + 2, b);
+      if constexpr (MODE < 2) read_x(kb + 1, 0, b);
+    });
   };
   load_scales(0);
-  copy_w(0, 0); copy_x(0, 0); copy_w(0, 1); copy_x(0, 1);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) copy(0, i);
   if (slabs > 1) {
-    copy_w(1, 0); copy_x(1, 0); copy_w(1, 1); copy_x(1, 1);
-    wait_vmcnt<12>();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) copy(1, i);
+    copy_barrier<8>();
   } else {
-    wait_vmcnt<0>();
+    copy_barrier<0>();
   }
-  slot_end();
   read_w(0, 0);
-  __builtin_amdgcn_sched_barrier(0);
-  wait_lgkm0();
-  slot_end();                    // every wave has read the quarter that the first read slot refills
-  if (wm == 1) slot_end();       // the second wave row runs one slot behind
+#pragma unroll
+  for (int b = 0; b < 8; ++b) read_x(0, 0, b);
   int kb = 0;
-  for (; kb + 2 < slabs; ++kb) stage(kb, I0{});
-  if (slabs > 1) stage(kb++, I1{});
-  stage(kb, I2{});
-  if (wm == 0) slot_end();
+  for (; kb + 2 < slabs; ++kb) slab(kb, I0{});
+  if (slabs > 1) slab(kb++, I1{});
+  slab(kb, I2{});
 
   // Y: each wave's blocks of 32 tokens x 64 features through a region of LDS of its own
   constexpr int OUT = out16_bytes<4, 2>();
