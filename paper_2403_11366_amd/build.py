@@ -34,13 +34,18 @@ FLAGS = [
     "-Wall", "-Wno-unused-result", "-Wno-unused-function",
 ]
 
+# Workgroups that LDS limits to one wave a SIMD have twice the registers, and the
+# compiler then moves the 4-bit tiles' sums to accumulation registers and back
+# around every product; this keeps them in vector registers.
+SOURCE_FLAGS = {"lora_mx4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD, os.path.basename(src) + ".o")
     # HIP sources keep their intermediate files (-save-temps=obj): the device
     # object is assembled from the saved gfx950 assembly, which asm_check reads.
     lang = ["-x", "hip", "-save-temps=obj"] if src.endswith(".hip") else []
-    cmd = [hipcc()] + FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC] + lang + \
+    cmd = [hipcc()] + FLAGS + SOURCE_FLAGS.get(src, []) + ["-I", os.path.join(ROOT, "include"), "-I", CSRC] + lang + \
           ["-c", os.path.join(CSRC, src), "-o", obj]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:

@@ -105,6 +105,94 @@ struct Mx4FwdArgs {
   int64_t m, n, k;
 };
 
+// Kernel of the 4-bit forward.  One launch that quantises X on its way for very
+// few values of X; else X is quantised before, and the product is formed by
+// waves on different slabs straight from memory (few tokens) or by tiles staged
+// in LDS.
+enum Mx4Kind {
+  MX4_TOKEN_8, MX4_TOKEN_2, MX4_FEW_1, MX4_FEW_2, MX4_FEW_4, MX4_64x128, MX4_128x128, MX4_256x128, MX4_256x256
+};
+
+struct Mx4Plan {
+  Mx4Kind kind;
+  int tiles_m, tiles_n;   // of the output
+  int64_t grid;           // workgroups
+  int block;
+};
+
+// LDS of the one launch: X's fragments and scales, the waves' sums.
+constexpr int kTokenRows = 16;
+inline size_t mx4_token_lds(int64_t slabs) { return (size_t)slabs * 2176 + 8192; }
+
+// The one launch up to 2^15 values of X: each workgroup quantises all of them
+// (8 x 4096 x 4096 7.2 us against 7.9 in two launches, 16 x 4096 x 4096 10.2
+// against 8.2; 1 x 4096 x 4096 4.7 against 7.5).
+//
+// The others by their estimated time in us, launches and the quantisation left
+// out.  A round of workgroups that fills the compute units takes c + full x slabs
+// and a round of few of them c + light x slabs (the card is then short of
+// neither power nor memory); the last one lies between.  Fitted to k = 512 to
+// 16384: 4096 x 4096 x 4096 36 us on 256 x 256 (58 on 256 x 128), 2048 x 4096 x
+// 4096 24 on 256 x 128 (32), 1024 x 4096 x 4096 15 on 128 x 128 (20), 512 x 4096
+// x 4096 11 on 64 x 128 (12), 128 x 4096 x 4096 9 from memory (10).
+struct Mx4Tile {
+  Mx4Kind kind;
+  int bm, bn, per_cu, block;
+  double c, light, full;
+};
+constexpr Mx4Tile kMx4Tiles[4] = {{MX4_256x256, 256, 256, 1, 512, 6.0, 1.37, 1.85},
+                                  {MX4_256x128, 256, 128, 1, 512, 5.0, 0.75, 1.2},
+                                  {MX4_128x128, 128, 128, 1, 256, 2.2, 0.6, 0.78},
+                                  {MX4_64x128, 64, 128, 2, 128, 1.5, 0.5, 0.93}};
+
+inline Mx4Plan mx4_plan_of(Mx4Kind kind, int64_t m, int64_t n, int bm, int bn, int block) {
+  Mx4Plan p;
+  p.kind = kind;
+  p.tiles_m = (int)((m + bm - 1) / bm);
+  p.tiles_n = (int)((n + bn - 1) / bn);
+  p.grid = (int64_t)p.tiles_m * p.tiles_n;
+  p.block = block;
+  return p;
+}
+
+inline Mx4Plan plan_mx4_fwd(int64_t m, int64_t n, int64_t k) {
+  const int64_t slabs = mx4_slabs(k), groups = (n + 15) / 16;
+  if (m <= kTokenRows && m * k <= (1 << 15) && mx4_token_lds(slabs) <= 160 * 1024) {
+    // eight waves share a group of 16 features while that leaves no compute unit a
+    // second round, else two (1 x 32000 x 4096 14 us, 17 with eight; 1 x 4096 x 4096
+    // 7.3, 4.7 with eight)
+    const bool eight = groups <= 384;
+    return mx4_plan_of(eight ? MX4_TOKEN_8 : MX4_TOKEN_2, 1, n, 1, eight ? 16 : 64, 512);
+  }
+  Mx4Plan best{};
+  double best_time = 1e30;
+  auto consider = [&](const Mx4Plan& p, double t) {
+    if (t < best_time) {
+      best_time = t;
+      best = p;
+    }
+  };
+  const double s = (double)slabs;
+  for (const Mx4Tile& t : kMx4Tiles) {
+    const Mx4Plan p = mx4_plan_of(t.kind, m, n, t.bm, t.bn, t.block);
+    const int64_t cap = 256 * t.per_cu, rounds = (p.grid + cap - 1) / cap, last = p.grid - (rounds - 1) * cap;
+    const double part = t.per_cu == 1 ? (double)last / 256 : (last > 256 ? 1.0 : 0.0);
+    consider(p, (double)(rounds - 1) * (t.c + t.full * s) + t.c + (t.light + (t.full - t.light) * part) * s);
+  }
+  // from memory: by the rounds of 256 workgroups, shared where several fit a compute unit
+  if (m <= 16) {
+    const Mx4Plan p = mx4_plan_of(MX4_FEW_1, m, n, 16, 16, 512);
+    consider(p, 1.0 + 0.15 * s * (p.grid > 256 ? (double)p.grid / 256 : 1.0));
+  } else if (m <= 32) {
+    const Mx4Plan p = mx4_plan_of(MX4_FEW_2, m, n, 32, 16, 512);
+    consider(p, 1.0 + 0.19 * s * (p.grid > 256 ? (double)p.grid / 256 : 1.0));
+  } else {
+    const Mx4Plan p = mx4_plan_of(MX4_FEW_4, m, n, 64, 32, 512);
+    consider(p, (double)((p.grid + 255) / 256) * (2.3 + 0.39 * s));
+  }
+  return best;
+}
+
 // Workspace of the 4-bit forward: X's codes and scales.
 struct Mx4Layout {
   size_t xc, xs, total;
