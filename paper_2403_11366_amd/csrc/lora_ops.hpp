@@ -9,6 +9,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace lora {
 
 constexpr int kMaxTop = 128;   // alternatives of a row, and entries of a teacher's list
@@ -27,12 +29,16 @@ struct RowShape {
 inline RowShape row_shape(int64_t vocab, int elem) {
   const int64_t chunks = (vocab * elem + 15) / 16;
   if (chunks <= 1024) return RowShape{256, 4};
-  if (chunks <= 2048) return RowShape{256, 8};
-  if (chunks <= 4096) return RowShape{512, 8};
+  if (chunks <= 2048) return RowShape{512, 4};
+  if (chunks <= 4096) return RowShape{1024, 4};
   if (chunks <= 8192) return RowShape{1024, 8};
   if (chunks <= 16384) return RowShape{1024, 16};
   return RowShape{1024, 0};
 }
+
+// Threads to a row in the calls that only read: many rows take small workgroups,
+// eight to a compute unit, few rows large ones.
+inline int read_threads(int64_t rows) { return rows > 768 ? 256 : 1024; }
 
 struct LogprobArgs {
   const void* logits;
@@ -48,11 +54,33 @@ struct LogprobArgs {
   int vocab, top;
 };
 
+// Units of 4 KiB of a row (and one for its ends), each with three fp32 sums.
+constexpr int kUnitBytes = 4096;
+constexpr int kMaxUnits = 1026;      // of 2^20 fp32 values
+inline int64_t score_units(int64_t vocab, int elem) { return (vocab * elem + kUnitBytes - 1) / kUnitBytes + 1; }
+// Parts of a row: workgroups of at least 16 units (one to a wave), as many as 256
+// together, with at most kMaxKeys top values to join.
+constexpr int kMaxKeys = 512;
+inline int score_parts(int64_t rows, int64_t vocab, int elem, int64_t top) {
+  const int64_t most = std::min<int64_t>(256 / rows, (score_units(vocab, elem) - 1) / 16);
+  return (int)std::max<int64_t>(1, top > 0 ? std::min<int64_t>(most, kMaxKeys / top) : most);
+}
+struct Unit {
+  float m, s, a;   // maximum, and two sums against it
+};
+struct ScoreParts {   // the workspace of a split call
+  uint64_t* keys;     // [rows, parts, top]
+  Unit* units;        // [rows, units_ld]
+  int64_t units_ld;
+  ScoreParts(char* ws, int64_t rows, int64_t vocab, int elem, int parts, int64_t top)
+      : keys(reinterpret_cast<uint64_t*>(ws)),
+        units(reinterpret_cast<Unit*>(ws + rows * parts * top * 8)),
+        units_ld(score_units(vocab, elem)) {}
+};
+// (for fp32 logits, which have more of both; never 0)
 inline size_t logprobs_workspace(int64_t rows, int64_t vocab, int64_t top) {
-  (void)rows;
-  (void)vocab;
-  (void)top;
-  return 256;
+  const int parts = score_parts(rows, vocab, 4, top);
+  return parts == 1 ? 256 : (size_t)rows * (score_units(vocab, 4) * sizeof(Unit) + 8 * parts * top);
 }
 
 struct DistillArgs {
