@@ -171,14 +171,13 @@ __device__ __forceinline__ float shift_of(float m) { return m == kNegInf ? 0.f :
 // Term::add(d, s, a) with d = z - shift, and Term::moved(d, s, a) moves both sums
 // to a shift that is larger by -d.
 // The units first .. last-1 of a row, unit u to box[u - first]; `wave` of `waves`.
-// Returns the largest value that this thread saw.
-template <typename T, typename Term>
-__device__ __forceinline__ float row_units(const Row<T>& row, int first, int last, int wave, int waves,
-                                           const Term& term, Unit* box) {
+// seen(i, m): the lane's own maximum of its i-th unit.
+template <typename T, typename Term, typename Seen>
+__device__ __forceinline__ void row_units(const Row<T>& row, int first, int last, int wave, int waves, const Term& term,
+                                          Unit* box, Seen&& seen) {
   constexpr int CH = Chunk<T>::CH, U = kUnitChunks / 64;
   const int lane = threadIdx.x & 63;
-  float own = kNegInf;
-  for (int u = first + wave; u < last; u += waves) {
+  for (int u = first + wave, it = 0; u < last; u += waves, ++it) {
     int4v v[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -190,7 +189,7 @@ __device__ __forceinline__ float row_units(const Row<T>& row, int first, int las
     for (int i = 0; i < U; ++i)
 #pragma unroll
       for (int e = 0; e < CH; ++e) m = fmaxf(m, Chunk<T>::get(v[i], e));
-    own = fmaxf(own, m);
+    seen(it, m);
     m = wave_max(m);
     const float shift = shift_of(m);
     float s = 0.f, a = 0.f;
@@ -202,7 +201,6 @@ __device__ __forceinline__ float row_units(const Row<T>& row, int first, int las
     a = wave_sum(a);
     if (lane == 0) box[u - first] = Unit{m, s, a};
   }
-  return own;
 }
 
 // The row's single elements as a unit, by the first wave.
@@ -274,13 +272,15 @@ __device__ __forceinline__ float value_of(uint32_t o) {
   return __builtin_bit_cast(float, o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
 constexpr int kCandidates = 512;
-constexpr int kOwners = 256;
+constexpr int kOwners = 512;
+constexpr int kSeen = 8;        // places of a thread for the maxima of its units
 
 template <int NT>
 struct TopShared {
   uint32_t maxima[NT];          // the threads' maxima in order_of form, 0: no value
   uint64_t cand[kCandidates];   // order above ~index: larger is earlier
-  int owner[kOwners];
+  uint16_t seen[kSeen * NT];    // their upper halves, unit by unit (wide rows: 2^by units a place)
+  int owner[kOwners];           // places of `seen` that reach the bound
   uint32_t bound;
   int count, owners;
   int part[2][16][NT / 64];
@@ -412,33 +412,40 @@ __device__ __forceinline__ void select_by_counting(const T* p, int col0, int col
 // least `top`.  After the barrier that publishes sh.bound, sh.count = 0 and
 // sh.owners = 0.
 template <typename T, int NT>
-__device__ __forceinline__ void select_top(const Row<T>& row, int first, int last, int col0, int col1, int edge, int top,
-                                           TopShared<NT>& sh) {
+__device__ __forceinline__ void select_top(const Row<T>& row, int first, int last, int by, int col0, int col1, int edge,
+                                           int top, TopShared<NT>& sh) {
   constexpr int CH = Chunk<T>::CH, kWaves = NT / 64, U = kUnitChunks / 64;
   const int tid = threadIdx.x;
   const uint32_t bound = sh.bound;
-  if (sh.maxima[tid] >= bound && sh.maxima[tid]) {
-    const int at = atomicAdd(&sh.owners, 1);
-    if (at < kOwners) sh.owner[at] = tid;
-  }
+  for (int i = 0; i < kSeen && (first + (i << by) * kWaves + (tid >> 6)) < last; ++i)
+    if (sh.seen[i * NT + tid] >= bound >> 16) {
+      const int at = atomicAdd(&sh.owners, 1);
+      if (at < kOwners) sh.owner[at] = i * NT + tid;
+    }
   if (edge >= 0) {
     const uint32_t o = order_of(row.value(edge));
     if (o >= bound) push<NT>(sh, o, edge);
   }
   __syncthreads();
   const int owners = sh.owners;
-  const int each = (last - first + kWaves - 1) / kWaves * U;     // chunks of an owner
+  // (a NaN passes the comparison, and ranks with -inf)
+  const float least = bound ? value_of(bound) : kNegInf;
   if (owners <= kOwners)
-    for (int q = tid >> 4; q < owners; q += NT / 16) {
-      const int t = sh.owner[q], c0 = (first + (t >> 6)) * kUnitChunks + (t & 63);
-      for (int j = tid & 15; j < each; j += 16) {
-        const int c = c0 + j / U * (kWaves * kUnitChunks) + j % U * 64;
-        if (c >= min(row.chunks, last * kUnitChunks)) continue;
+    for (int q = tid / U; q < owners; q += NT / U) {
+      const int place = sh.owner[q], t = place % NT;
+      for (int k = 0; k < 1 << by; ++k) {
+        const int u = first + ((place / NT << by) + k) * kWaves + (t >> 6);
+        const int c = u * kUnitChunks + (t & 63) + tid % U * 64;
+        if (u >= last || c >= row.chunks) break;
         const int4v v = row.at(c);
+        uint32_t in = 0;
 #pragma unroll
-        for (int e = 0; e < CH; ++e) {
-          const uint32_t o = order_of(Chunk<T>::get(v, e));
-          if (o >= bound) push<NT>(sh, o, row.head + c * CH + e);
+        for (int e = 0; e < CH; ++e) in |= !(Chunk<T>::get(v, e) < least) ? 1u << e : 0u;
+        for (; in; in &= in - 1) {
+          const int e = __builtin_ctz(in), h = e / (CH / 4);
+          int4v x;
+          x[0] = h < 2 ? (h == 0 ? v[0] : v[1]) : (h == 2 ? v[2] : v[3]);
+          push<NT>(sh, order_of(CH == 4 || !(e & 1) ? Chunk<T>::get(x, 0) : Chunk<T>::get(x, 1)), row.head + c * CH + e);
         }
       }
     }
@@ -485,7 +492,7 @@ __global__ __launch_bounds__(NT) void lora_logprobs_kernel(const T* __restrict__
                                                            int32_t* __restrict__ top_ids, float* __restrict__ top_logp,
                                                            int vocab, int top, int parts, ScoreParts ws) {
   __shared__ TopShared<NT> sh;
-  __shared__ Unit box[SPLIT ? 1 : kMaxUnits];
+  __shared__ Unit box[SPLIT ? 1 : (NT == 256 ? kSmallUnits : kMaxUnits)];
   const int64_t r = SPLIT ? blockIdx.x / (unsigned)parts : blockIdx.x;
   const int part = SPLIT ? (int)(blockIdx.x - (unsigned)r * (unsigned)parts) : 0;
   const int tid = threadIdx.x;
@@ -497,7 +504,15 @@ __global__ __launch_bounds__(NT) void lora_logprobs_kernel(const T* __restrict__
   int edge = row.edge(vocab);
   const float xe = row.value(edge);
   Unit* out = SPLIT ? ws.units + r * ws.units_ld : box;
-  const float own = row_units(row, first, last, uniform(tid >> 6), NT / 64, term, out + first);
+  int by = 0;
+  while ((last - first - 1) / (NT / 64) >> by >= kSeen) ++by;
+  float own = kNegInf, place = kNegInf;
+  row_units(row, first, last, uniform(tid >> 6), NT / 64, term, out + first, [&](int i, float m) LORA_INLINE {
+    if (top == 0) return;
+    own = fmaxf(own, m);
+    place = (i & ((1 << by) - 1)) == 0 ? m : fmaxf(place, m);
+    sh.seen[(i >> by) * NT + tid] = (uint16_t)(order_of(place) >> 16);
+  });
   if (part == 0 && tid < 64) edge_unit(xe, term, out + units);
   if (top > 0) {   // 0 for the threads without a chunk
     sh.maxima[tid] = (first + (tid >> 6)) * kUnitChunks + (tid & 63) < min(row.chunks, last * kUnitChunks) ? order_of(own) : 0u;
@@ -514,7 +529,7 @@ __global__ __launch_bounds__(NT) void lora_logprobs_kernel(const T* __restrict__
     const int col1 = part == parts - 1 ? vocab : row.head + last * kUnitChunks * Chunk<T>::CH;
     if (edge < col0 || edge >= col1) edge = -1;
     __syncthreads();
-    select_top<T, NT>(row, first, last, col0, col1, edge, top, sh);
+    select_top<T, NT>(row, first, last, by, col0, col1, edge, top, sh);
     const int n = sh.count;
     uint64_t* keys = ws.keys + (r * parts + part) * top;
     for (int c = tid; c < n; c += NT) {
@@ -527,7 +542,7 @@ __global__ __launch_bounds__(NT) void lora_logprobs_kernel(const T* __restrict__
     if (tid == 0) put_scores(row, sc, u, tokens, r, logp, entropy, vocab);
     if (top == 0) return;
     __syncthreads();
-    select_top<T, NT>(row, 0, units, 0, vocab, edge, top, sh);
+    select_top<T, NT>(row, 0, units, by, 0, vocab, edge, top, sh);
     const int n = sh.count;
     for (int c = tid; c < n; c += NT) {
       const uint64_t mine = sh.cand[c];
@@ -757,7 +772,7 @@ template <int H, int NT, typename T>
 __device__ __forceinline__ Unit row_sums(const Row<T>& row, float xe, float scale, Unit* box) {
   const DistillTerm<H> term{scale};
   const int units = row.units();
-  row_units(row, 0, units, uniform((int)threadIdx.x >> 6), NT / 64, term, box);
+  row_units(row, 0, units, uniform((int)threadIdx.x >> 6), NT / 64, term, box, [](int, float) LORA_INLINE {});
   if (threadIdx.x < 64) edge_unit(xe, term, box + units);
   __syncthreads();
   Unit u = join_units(box, units + 1, term);
@@ -996,14 +1011,16 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     }
     const int edge = row.edge(vocab);
     if (edge >= 0) dz[edge] = Chunk<T>::pack1(gr.template dense<H>(xe));
-    // (a thread's two entries may have one column, more are looked for in the list)
-    const int k0 = sh.first[tid], k1 = k0 >= 0 ? sh.next[k0] : -1;
-    const bool few = k1 < 0 || sh.next[k1] < 0;
-    for (int k = k0; k >= 0; k = sh.next[k]) {
+    for (int k = sh.first[tid]; k >= 0; k = sh.next[k]) {
       const int id = sh.list.id[k];
-      float p = sh.list.p[k];
-      if (!few) p = listed_p(sh.list, id, top);
-      else if (k1 >= 0 && sh.list.id[k0] == sh.list.id[k1]) p = sh.list.p[k0] + sh.list.p[k1];
+      float p = 0.f;      // (the sum of two is the same in either order, the list has that of more)
+      int same = 0;
+      for (int j = sh.first[tid]; j >= 0; j = sh.next[j])
+        if (sh.list.id[j] == id) {
+          p += sh.list.p[j];
+          ++same;
+        }
+      if (same > 2) p = listed_p(sh.list, id, top);
       dz[id] = Chunk<T>::pack1(empty ? 0.f : listed_grad<H>(sh.list, id, p, sh.x[k], top, g, tau, w, gr));
     }
     if (tid < 64) {
@@ -1104,15 +1121,16 @@ hipError_t launch_token_logprobs(const LogprobArgs& a, hipStream_t st) {
       const hipError_t e = launch(lora_logprobs_kernel<T, 1024, true>, 1024, a.rows * parts);
       return e != hipSuccess ? e : launch(lora_logprobs_join_kernel<T>, kMaxKeys, a.rows);
     }
-    return read_threads(a.rows) == 256 ? launch(lora_logprobs_kernel<T, 256, false>, 256, a.rows)
-                                       : launch(lora_logprobs_kernel<T, 1024, false>, 1024, a.rows);
+    return with_int<256, 512, 1024>(read_threads(a.rows, a.vocab, sizeof(T), 4), [&](auto nt) {
+      return launch(lora_logprobs_kernel<T, decltype(nt)::value, false>, decltype(nt)::value, a.rows);
+    });
   });
 }
 
 hipError_t launch_distill_fwd(const DistillArgs& a, hipStream_t st) {
   return with_type(a.f32, [&](auto t) {
     using T = decltype(t);
-    return with_int<256, 1024>(read_threads(a.rows), [&](auto nt) {
+    return with_int<256, 512, 1024>(read_threads(a.rows, a.vocab, sizeof(T), 1), [&](auto nt) {
       constexpr int NT = decltype(nt)::value;
       hipLaunchKernelGGL((lora_distill_fwd_kernel<T, NT>), dim3((unsigned)a.rows), dim3(NT), 0, st,
                          static_cast<const T*>(a.logits), a.ld, a.ids, a.teacher, a.labels, a.tau, a.w, a.loss,

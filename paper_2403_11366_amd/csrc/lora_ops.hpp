@@ -36,9 +36,23 @@ inline RowShape row_shape(int64_t vocab, int elem) {
   return RowShape{1024, 0};
 }
 
-// Threads to a row in the calls that only read: many rows take small workgroups,
-// eight to a compute unit, few rows large ones.
-inline int read_threads(int64_t rows) { return rows > 768 ? 256 : 1024; }
+// Units of 4 KiB of a row (and one for its ends), each with three fp32 sums.
+constexpr int kUnitBytes = 4096;
+constexpr int kMaxUnits = 1026;      // of 2^20 fp32 values
+constexpr int kSmallUnits = 33;      // of the rows that 256 threads take
+inline int64_t score_units(int64_t vocab, int elem) { return (vocab * elem + kUnitBytes - 1) / kUnitBytes + 1; }
+
+// Threads to a row in the calls that only read it; a row's results do not depend
+// on them.  Few rows take 1024 threads each.  Otherwise a wave is to have units
+// to load while others reduce, but not so many that few rows leave the chip empty:
+// the forward's waves more than one unit (4096 x 32000 bf16: 48 us with 512
+// threads, 54 with 256; 8192 x 8000: 41 and 32), those of the log probabilities,
+// where a row's threads wait for its selection, more than four (4096 x 32000 with 20
+// alternatives: 78 and 67; 777 x 50021 fp32 with 64: 52 and 56).
+inline int read_threads(int64_t rows, int64_t vocab, int elem, int least_units) {
+  if (rows <= 256) return 1024;
+  return rows <= 768 || score_units(vocab, elem) > std::min(8 * least_units, kSmallUnits) ? 512 : 256;
+}
 
 struct LogprobArgs {
   const void* logits;
@@ -54,10 +68,6 @@ struct LogprobArgs {
   int vocab, top;
 };
 
-// Units of 4 KiB of a row (and one for its ends), each with three fp32 sums.
-constexpr int kUnitBytes = 4096;
-constexpr int kMaxUnits = 1026;      // of 2^20 fp32 values
-inline int64_t score_units(int64_t vocab, int elem) { return (vocab * elem + kUnitBytes - 1) / kUnitBytes + 1; }
 // Parts of a row: workgroups of at least 16 units (one to a wave), as many as 256
 // together, with at most kMaxKeys top values to join.
 constexpr int kMaxKeys = 512;
