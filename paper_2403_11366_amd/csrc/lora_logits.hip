@@ -679,7 +679,7 @@ __device__ __forceinline__ float row_loss(const ListShared& sh, X&& x, int top, 
 // How the two softmaxes' exponentials of an element are formed from u = 2^((z -
 // max z) scale): one where the temperature is 1 or a term has no weight, a power
 // of u at temperatures 2 and 4, else an exponential of its own (4096 x 32000
-// bf16: the step 113 us with one exponential an element, 124 with two).
+// bf16: the step takes 98 us at temperatures 1, 2 and 4, 134 at 3).
 enum Hard { HARD_SAME, HARD_SQUARE, HARD_FOURTH, HARD_OWN };
 __host__ __device__ __forceinline__ Hard hard_of(float tau, float w) {
   if (tau == 1.f || w == 1.f || w == 0.f) return HARD_SAME;

@@ -40,8 +40,8 @@ __device__ __forceinline__ uint32_t quantise_piece(const int4v& x, int& scale) {
     const uint32_t w = (uint32_t)x[h] & 0x7FFF7FFFu;
     top = max(top, max(w & 0xFFFFu, w >> 16));
   }
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xf, 0xf, true));   // lane ^ 1
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xf, 0xf, true));   // lane ^ 2
   const int field = (int)(top >> 7);
   const bool nan = field == 255;
   scale = nan ? 255 : max(field - 2, 0);
@@ -59,51 +59,57 @@ __device__ __forceinline__ uint32_t quantise_piece(const int4v& x, int& scale) {
 }
 
 // ---------------------------------------------------------------------------
-// Quantisation.  A workgroup takes a cell of scales, 64 rows x 256 columns: four
-// lanes a block, each 8 columns.  Reads 2 bytes and writes 0.53 a column; bound
-// by HBM.
+// Quantisation.  A workgroup takes 16 rows x 256 columns, a quarter of a cell of
+// scales: four rows and those 16, 32 and 48 after them, whose scales stand
+// together.  Four lanes a block, each 8 columns.  Reads 2 bytes and writes 0.53 a
+// column; bound by HBM.
 __global__ __launch_bounds__(256) void lora_mx4_quantize_kernel(const u16* __restrict__ X, uint8_t* __restrict__ codes,
                                                                 uint8_t* __restrict__ scales, int rows, int k,
                                                                 int slabs, int groups) {
-  __shared__ __attribute__((aligned(16))) uint8_t cell[512];
-  const int slab = (int)blockIdx.x % slabs, grp = (int)blockIdx.x / slabs;
+  __shared__ __attribute__((aligned(16))) uint8_t cell[128];   // [block & 3][32]
+  const int slab = (int)blockIdx.x % slabs, quarter = (int)blockIdx.x / slabs, grp = quarter >> 2;
   const int tid = threadIdx.x, piece = tid & 31, col = slab * 256 + 8 * piece;
   const bool inside = col < k;
-  int4v x[8];
+  int4v x[2];
+  int lrow[2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = grp * 64 + (tid >> 5) + 8 * i;
+  for (int i = 0; i < 2; ++i) {
+    const int r = (tid >> 5) + 8 * i;
+    lrow[i] = 4 * (quarter & 3) + (r & 3) + 16 * (r >> 2);
+    const int row = grp * 64 + lrow[i];
     x[i] = inside && row < rows ? *reinterpret_cast<const int4v*>(X + (size_t)row * k + col) : int4v{0, 0, 0, 0};
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int lrow = (tid >> 5) + 8 * i, row = grp * 64 + lrow;
+  for (int i = 0; i < 2; ++i) {
+    const int row = grp * 64 + lrow[i];
     int scale;
     const uint32_t out = quantise_piece(x[i], scale);
-    const int block = slab * 8 + (piece >> 2);
-    if ((piece & 3) == 0) cell[mx4_scale_offset(lrow, block)] = (uint8_t)(row < rows && block * 32 < k ? scale : 0);
+    const int block = slab * 8 + (piece >> 2), at = mx4_scale_offset(lrow[i], block);
+    if ((piece & 3) == 0) cell[(at >> 7) * 32 + (at & 31)] = (uint8_t)(row < rows && block * 32 < k ? scale : 0);
     if (row < rows) *reinterpret_cast<uint32_t*>(codes + ((size_t)row * slabs + slab) * 128 + piece * 4) = out;
   }
   __syncthreads();
   if (tid < 32)
-    reinterpret_cast<int4v*>(scales + ((size_t)slab * groups + grp) * 512)[tid] = reinterpret_cast<const int4v*>(cell)[tid];
+    *reinterpret_cast<uint32_t*>(scales + ((size_t)slab * groups + grp) * 512 + (tid >> 3) * 128 + (quarter & 3) * 32 +
+                                 (tid & 7) * 4) = reinterpret_cast<const uint32_t*>(cell)[tid];
 }
 
-// The values of codes and scales: a lane takes 8 columns.
+// The values of codes and scales: a lane takes 8 columns of two rows, a workgroup
+// 16 rows x 256 columns.
 __global__ __launch_bounds__(256) void lora_mx4_dequantize_kernel(const uint8_t* __restrict__ codes,
                                                                   const uint8_t* __restrict__ scales,
                                                                   u16* __restrict__ X, int rows, int k, int slabs,
                                                                   int groups) {
-  const int slab = (int)blockIdx.x % slabs, grp = (int)blockIdx.x / slabs;
+  const int slab = (int)blockIdx.x % slabs, r0 = (int)blockIdx.x / slabs * 16, grp = r0 >> 6;
   const int tid = threadIdx.x, piece = tid & 31, col = slab * 256 + 8 * piece, block = slab * 8 + (piece >> 2);
   if (col >= k) return;
   const uint8_t* cell = scales + ((size_t)slab * groups + grp) * 512;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int lrow = (tid >> 5) + 8 * i, row = grp * 64 + lrow;
+  for (int i = 0; i < 2; ++i) {
+    const int row = r0 + (tid >> 5) + 8 * i;
     if (row >= rows) continue;
     const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + ((size_t)row * slabs + slab) * 128 + piece * 4);
-    const int s = cell[mx4_scale_offset(lrow, block)];
+    const int s = cell[mx4_scale_offset(row & 63, block)];
     // 2^(s - 127); s = 0 is a subnormal, 255 NaN
     const uint32_t bits = s == 0 ? 0x00400000u : (s == 255 ? 0x7FC00000u : (uint32_t)s << 23);
     const float unit = __builtin_bit_cast(float, bits);
@@ -502,7 +508,7 @@ __global__ __launch_bounds__(64 * WM * WN) void lora_mx4_kernel(
 
 hipError_t launch_mx4_quantize(const Mx4QuantArgs& a, hipStream_t st) {
   const int slabs = (int)mx4_slabs(a.k), groups = (int)mx4_groups(a.rows);
-  hipLaunchKernelGGL(lora_mx4_quantize_kernel, dim3((unsigned)(slabs * groups)), dim3(256), 0, st, a.X, a.codes, a.scales,
+  hipLaunchKernelGGL(lora_mx4_quantize_kernel, dim3((unsigned)(slabs * groups * 4)), dim3(256), 0, st, a.X, a.codes, a.scales,
                      (int)a.rows, (int)a.k, slabs, groups);
   return hipGetLastError();
 }
@@ -510,7 +516,7 @@ hipError_t launch_mx4_quantize(const Mx4QuantArgs& a, hipStream_t st) {
 hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, uint16_t* X, int64_t rows, int64_t k,
                                  hipStream_t st) {
   const int slabs = (int)mx4_slabs(k), groups = (int)mx4_groups(rows);
-  hipLaunchKernelGGL(lora_mx4_dequantize_kernel, dim3((unsigned)(slabs * groups)), dim3(256), 0, st, codes, scales, X,
+  hipLaunchKernelGGL(lora_mx4_dequantize_kernel, dim3((unsigned)(slabs * groups * 4)), dim3(256), 0, st, codes, scales, X,
                      (int)rows, (int)k, slabs, groups);
   return hipGetLastError();
 }
