@@ -4,6 +4,7 @@
 // leaves its outputs untouched.
 #include <cmath>
 #include <stdint.h>
+#include <string.h>
 
 #include "lora_linear.h"
 #include "lora_ops.hpp"
@@ -28,7 +29,16 @@ Range span(const void* p, uint64_t bytes) {
 bool aligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 bool aligned16(const void* p) { return aligned(p, 16); }
 bool aligned4(const void* p) { return aligned(p, 4); }
-unsigned elem_bytes(lora_dtype dtype) { return dtype == LORA_F32 ? 4 : 2; }
+// A C caller may pass any int as the type: its bits are read as an int (loading
+// a lora_dtype that holds a value past the enumerators is undefined in C++).
+int code_of(const lora_dtype* dtype) {
+  static_assert(sizeof(lora_dtype) == sizeof(int), "lora_dtype is int-sized");
+  int code;
+  memcpy(&code, dtype, sizeof code);
+  return code;
+}
+
+unsigned elem_bytes(int dtype) { return dtype == LORA_F32 ? 4 : 2; }
 
 // True if an output overlaps an input or another output.  Empty ranges
 // (arguments that a call does without) overlap nothing.
@@ -73,12 +83,12 @@ lora_status check_logits(int64_t rows, int64_t vocab, int64_t ld, int64_t top) {
 }
 
 // Bytes from the first row's start to the last row's end.
-uint64_t logits_bytes(int64_t rows, int64_t vocab, int64_t ld, lora_dtype dtype) {
+uint64_t logits_bytes(int64_t rows, int64_t vocab, int64_t ld, int dtype) {
   return (uint64_t)((rows - 1) * ld + vocab) * elem_bytes(dtype);
 }
 
 // Checks that the three distillation calls share.
-lora_status check_distill(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* ids, const float* teacher,
+lora_status check_distill(const void* logits, int dtype, int64_t ld, const int32_t* ids, const float* teacher,
                           const int32_t* labels, float tau, float w, int64_t rows, int64_t vocab, int64_t top) {
   if (!logits || !ids || !teacher) return LORA_ERR_NULL;
   if (dtype != LORA_BF16 && dtype != LORA_F32) return LORA_ERR_UNSUPPORTED;
@@ -93,7 +103,7 @@ lora_status check_distill(const void* logits, lora_dtype dtype, int64_t ld, cons
   return LORA_OK;
 }
 
-lora::DistillArgs distill_args(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* ids,
+lora::DistillArgs distill_args(const void* logits, int dtype, int64_t ld, const int32_t* ids,
                                const float* teacher, const int32_t* labels, float tau, float w, int64_t rows,
                                int64_t vocab, int64_t top) {
   lora::DistillArgs a{};
@@ -178,10 +188,11 @@ size_t lora_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int64_t t
   return lora::logprobs_workspace(rows, vocab, top);
 }
 
-lora_status lora_token_logprobs(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* tokens,
+lora_status lora_token_logprobs(const void* logits, lora_dtype type, int64_t ld, const int32_t* tokens,
                                 float temperature, float* logp, float* entropy, int32_t* top_ids, float* top_logp,
                                 void* workspace, size_t workspace_bytes, int64_t rows, int64_t vocab, int64_t top,
                                 void* stream) {
+  const int dtype = code_of(&type);
   if (!logits || !entropy || (tokens != nullptr) != (logp != nullptr)) return LORA_ERR_NULL;
   if (dtype != LORA_BF16 && dtype != LORA_F32) return LORA_ERR_UNSUPPORTED;
   const lora_status st = check_logits(rows, vocab, ld, top);
@@ -205,9 +216,10 @@ lora_status lora_token_logprobs(const void* logits, lora_dtype dtype, int64_t ld
   return status_of(lora::launch_token_logprobs(a, reinterpret_cast<hipStream_t>(stream)));
 }
 
-lora_status lora_distill_fwd(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* teacher_ids,
+lora_status lora_distill_fwd(const void* logits, lora_dtype type, int64_t ld, const int32_t* teacher_ids,
                              const float* teacher_logits, const int32_t* labels, float temperature, float soft_weight,
                              float* loss, float* saved, int64_t rows, int64_t vocab, int64_t top, void* stream) {
+  const int dtype = code_of(&type);
   const lora_status st = check_distill(logits, dtype, ld, teacher_ids, teacher_logits, labels, temperature,
                                        soft_weight, rows, vocab, top);
   if (st != LORA_OK) return st;
@@ -226,10 +238,11 @@ lora_status lora_distill_fwd(const void* logits, lora_dtype dtype, int64_t ld, c
   return status_of(lora::launch_distill_fwd(a, reinterpret_cast<hipStream_t>(stream)));
 }
 
-lora_status lora_distill_bwd(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* teacher_ids,
+lora_status lora_distill_bwd(const void* logits, lora_dtype type, int64_t ld, const int32_t* teacher_ids,
                              const float* teacher_logits, const int32_t* labels, float temperature, float soft_weight,
                              const float* saved, const float* dloss, void* dlogits, int64_t rows, int64_t vocab,
                              int64_t top, void* stream) {
+  const int dtype = code_of(&type);
   const lora_status st = check_distill(logits, dtype, ld, teacher_ids, teacher_logits, labels, temperature,
                                        soft_weight, rows, vocab, top);
   if (st != LORA_OK) return st;
@@ -251,10 +264,11 @@ lora_status lora_distill_bwd(const void* logits, lora_dtype dtype, int64_t ld, c
   return status_of(lora::launch_distill_bwd(a, reinterpret_cast<hipStream_t>(stream)));
 }
 
-lora_status lora_distill_step(const void* logits, lora_dtype dtype, int64_t ld, const int32_t* teacher_ids,
+lora_status lora_distill_step(const void* logits, lora_dtype type, int64_t ld, const int32_t* teacher_ids,
                               const float* teacher_logits, const int32_t* labels, float temperature, float soft_weight,
                               const float* dloss, float* loss, void* dlogits, int64_t rows, int64_t vocab, int64_t top,
                               void* stream) {
+  const int dtype = code_of(&type);
   const lora_status st = check_distill(logits, dtype, ld, teacher_ids, teacher_logits, labels, temperature,
                                        soft_weight, rows, vocab, top);
   if (st != LORA_OK) return st;
