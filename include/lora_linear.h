@@ -52,10 +52,10 @@ typedef uint16_t lora_bf16;
 typedef enum {
   LORA_OK = 0,
   LORA_ERR_NULL = 1,        /* a required pointer is NULL */
-  LORA_ERR_SHAPE = 2,       /* m < 1, n or k < 8 or not a multiple of 8, r < 1, merge sign not +-1 */
-  LORA_ERR_ALIGN = 3,       /* a matrix pointer is not 16-byte aligned */
+  LORA_ERR_SHAPE = 2,       /* m < 1, n or k < 8 or not a multiple of 8, r < 1, merge sign not +-1, or a call's own rule */
+  LORA_ERR_ALIGN = 3,       /* a pointer is not aligned: a matrix to 16 bytes, others as the call says */
   LORA_ERR_UNSUPPORTED = 4, /* r > 64, or a dimension beyond the supported range */
-  LORA_ERR_WORKSPACE = 5,   /* workspace missing or smaller than lora_linear_bwd_workspace_size() */
+  LORA_ERR_WORKSPACE = 5,   /* workspace missing or smaller than the call's ..._workspace_size() */
   LORA_ERR_ALIAS = 6,       /* an output overlaps an input or another output */
   LORA_ERR_HIP = 7          /* the HIP runtime reported an error at launch; also returned, before anything
                                is enqueued, while an error of an earlier HIP call is pending on the calling

@@ -1,8 +1,8 @@
 // Internal interface of the operators around the layer's output between the C
 // ABI (lora_ops_abi.cpp: argument checks) and their kernels: 4-bit weights
 // (lora_mx4.hip), token log probabilities and distillation (lora_logits.hip).
-// Shapes here have already been validated; the launch rules stand here, so that
-// lora_linear_plan() reports the launches that the entry points make.
+// Shapes here have already been validated; the launch rules stand here, apart from
+// the kernels, so that they can be checked on the host.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -18,14 +18,16 @@ constexpr int kMaxTop = 128;   // alternatives of a row, and entries of a teache
 // ---- rows of logits ----------------------------------------------------------
 // A row is walked in chunks of 16 bytes (8 bf16 or 4 fp32 values): the whole
 // ones that start at a 16-byte boundary, and single elements before and after.
-// One workgroup takes a row; `threads` x `keep` chunks fit its registers, keep =
-// 0 reads the row again in every pass.
+//
+// The distillation step keeps a row in the registers of one workgroup: `threads`
+// x `keep` chunks; keep = 0 reads the row again for the gradient.
 struct RowShape {
   int threads, keep;
 };
 
-// The smallest workgroup whose registers hold the row, up to 64 of a thread's
-// 128 registers (1024 threads).
+// Four chunks a thread, with which it can hold the exponentials too, up to 1024
+// threads; then up to 16, 64 of a thread's 128 registers (512 x 131072 bf16 66 us, 81
+// read twice).
 inline RowShape row_shape(int64_t vocab, int elem) {
   const int64_t chunks = (vocab * elem + 15) / 16;
   if (chunks <= 1024) return RowShape{256, 4};
