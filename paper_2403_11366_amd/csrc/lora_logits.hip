@@ -94,6 +94,8 @@ struct Row {
     const int tid = threadIdx.x;
     return tid < head ? tid : (tid >= CH && tid - CH < vocab - tail0 ? tail0 + tid - CH : -1);
   }
+  // as stored: nothing waits for the load before the value is formed
+  __device__ __forceinline__ T raw(int index) const { return index >= 0 ? p[index] : Chunk<T>::pack1(kNegInf); }
   __device__ __forceinline__ float value(int index) const { return index >= 0 ? Chunk<T>::one(p[index]) : kNegInf; }
   static __device__ __forceinline__ int4v fill() {
     return int4v{Chunk<T>::kFill, Chunk<T>::kFill, Chunk<T>::kFill, Chunk<T>::kFill};
@@ -606,29 +608,32 @@ struct ListShared {
 };
 
 // A row's list and label as the first wave's lanes hold them: entries lane and
-// lane + 64, -1: none.
+// lane + 64, as loaded (nothing waits for the loads here).
 struct ListIn {
   int id[2], label;
   float t[2];
 };
-__device__ __forceinline__ ListIn list_in(const int32_t* ids, const float* t, const int32_t* label, int vocab, int top) {
+__device__ __forceinline__ ListIn list_in(const int32_t* ids, const float* t, const int32_t* label, int top) {
   const int lane = threadIdx.x & 63;
   ListIn in;
   in.label = label ? *label : -1;
-  if ((uint32_t)in.label >= (uint32_t)vocab) in.label = -1;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int k = lane + 64 * h;
     in.id[h] = k < top ? ids[k] : -1;
     in.t[h] = k < top ? t[k] : kNegInf;
-    if ((uint32_t)in.id[h] >= (uint32_t)vocab) in.id[h] = -1;
   }
   return in;
 }
 
-// One wave forms p and leaves it in sh (before a barrier of the caller).
-__device__ __forceinline__ void teacher_list(const ListIn& in, float scale, int top, ListShared& sh) {
+// One wave forms p and leaves it in sh (before a barrier of the caller); ids
+// outside the vocabulary are none (-1).
+__device__ __forceinline__ void teacher_list(ListIn in, float scale, int vocab, int top, ListShared& sh) {
   const int lane = threadIdx.x & 63;
+  if ((uint32_t)in.label >= (uint32_t)vocab) in.label = -1;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if ((uint32_t)in.id[h] >= (uint32_t)vocab) in.id[h] = -1;
   float y[2], e[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) y[h] = in.id[h] >= 0 ? in.t[h] : kNegInf;
@@ -802,7 +807,7 @@ __global__ __launch_bounds__(NT) void lora_distill_fwd_kernel(const T* __restric
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x;
   const Row<T> row(logits + r * ld, vocab);
-  if (tid < 64) teacher_list(list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, vocab, top), kLog2e / tau, top, list);
+  if (tid < 64) teacher_list(list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, top), kLog2e / tau, vocab, top, list);
   const float xe = row.value(row.edge(vocab));
   Unit sum;
   with_hard(hard_of(tau, w), [&](auto hc) LORA_INLINE {
@@ -850,7 +855,7 @@ __global__ __launch_bounds__(kGradThreads, 8) void lora_distill_bwd_kernel(
   int edge = row.edge(vocab);
   if (edge < col0 || edge >= col1) edge = -1;
   const float xe = row.value(edge);
-  if (tid < 64) teacher_list(list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, vocab, top), kLog2e / tau, top, list);
+  if (tid < 64) teacher_list(list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, top), kLog2e / tau, vocab, top, list);
   const float4 sv = saved[r];
   const float g = dloss[r];
   __syncthreads();
@@ -931,13 +936,15 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
   float held[kHold ? KEEP : 1][CH];
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) v[i] = load(i);
-  ListIn in = list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, vocab, top);
-  float xe = row.value(row.edge(vocab)), g = dloss[r];
+  ListIn in = list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, top);
+  T xe_in = row.raw(row.edge(vocab));
+  float g = dloss[r];
   for (int turn = 0;; turn ^= 1) {
     StepShared<NT>& sh = both[turn];
     T* dz = dlogits + r * ld;
-    if (tid < 64) teacher_list(in, kLog2e / tau, top, sh.list);
+    if (tid < 64) teacher_list(in, kLog2e / tau, vocab, top, sh.list);
     sh.first[tid] = -1;
+    const float xe = Chunk<T>::one(xe_in);
     float m = xe;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
@@ -950,7 +957,7 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     const float shift = shift_of(m);
     // the entries' columns: chained to the threads that store them
     const int mine = tid <= top ? sh.list.id[tid] : -1;
-    const float xl = row.value(mine);
+    const T xl = row.raw(mine);
     if (mine >= 0) {
       const int owner = mine < row.head ? mine : (mine >= row.tail0 ? CH + mine - row.tail0 : (mine - row.head) / CH % NT);
       sh.next[tid] = atomicExch(&sh.first[owner], tid);
@@ -961,8 +968,9 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     const int64_t rl = more ? rn : r;
     const Row<T> next(logits + rl * ld, vocab);
     rs = make_rsrc(uniform_ptr(next.p + next.head), more ? (uint64_t)uniform(next.chunks) * 16 : 0);
-    const ListIn in_next = list_in(ids + rl * top, teacher + rl * top, labels ? labels + rl : nullptr, vocab, top);
-    const float xe_next = next.value(next.edge(vocab)), g_next = dloss[rl];
+    const ListIn in_next = list_in(ids + rl * top, teacher + rl * top, labels ? labels + rl : nullptr, top);
+    const T xe_next = next.raw(next.edge(vocab));
+    const float g_next = dloss[rl];
     float soft = 0.f, hard = 0.f;
     auto add = [&](float x) LORA_INLINE {
       const float d = x - shift, u = exp2_hw(d * scale);
@@ -984,7 +992,7 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     }
     add(xe);
     if constexpr (H == HARD_SAME) hard = soft;
-    if (mine >= 0) sh.x[tid] = xl;   // (from here on dlogits may be written over the logits)
+    if (mine >= 0) sh.x[tid] = Chunk<T>::one(xl);   // (from here on dlogits may be written over the logits)
     const float2 sum = block_sum2<NT>(soft, hard, sh.sbox);
     const bool empty = sum.x == 0.f;
     const float inf = __builtin_inff();
@@ -1043,7 +1051,7 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     r = rn;
     row = next;
     in = in_next;
-    xe = xe_next;
+    xe_in = xe_next;
     g = g_next;
   }
 }
@@ -1068,7 +1076,7 @@ __global__ __launch_bounds__(NT) void lora_distill_wide_kernel(const T* logits, 
   const bool alike = lies_alike<T>(logits, dlogits);
   const Row<T> row(logits + r * ld, vocab);
   const float g = dloss[r];
-  if (tid < 64) teacher_list(list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, vocab, top), kLog2e / tau, top, list);
+  if (tid < 64) teacher_list(list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, top), kLog2e / tau, vocab, top, list);
   const int edge = row.edge(vocab);
   const float xe = row.value(edge);
   with_hard(hard_of(tau, w), [&](auto hc) LORA_INLINE {
