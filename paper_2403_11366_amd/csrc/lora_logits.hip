@@ -763,6 +763,35 @@ __device__ __forceinline__ float listed_grad(const ListShared& sh, int id, float
   return d;
 }
 
+// The listed columns of a row, chained to the threads that store their chunks: a
+// column's own gradient follows its dense one from the same thread, in its program
+// order, so no barrier waits for the stores.
+template <int NT>
+struct ListChain {
+  float x[kMaxTop + 1];         // the entries' logits
+  int next[kMaxTop + 1];        // a thread's entries, -1: end
+  int first[NT];
+  // (thread `owner` of the workgroup stores the column; all `first` are -1 before)
+  __device__ __forceinline__ void link(int k, int owner) { next[k] = atomicExch(&first[owner], k); }
+  template <int H, typename T>
+  __device__ __forceinline__ void put(T* dz, const ListShared& list, int top, bool empty, float g, float tau, float w,
+                                      const GradRow& gr) const {
+    const int k0 = first[threadIdx.x];
+    for (int k = k0; k >= 0; k = next[k]) {
+      const int id = list.id[k];
+      float p = 0.f;      // (the sum of two is the same in either order, the list has that of more)
+      int same = 0;
+      for (int j = k0; j >= 0; j = next[j])
+        if (list.id[j] == id) {
+          p += list.p[j];
+          ++same;
+        }
+      if (same > 2) p = listed_p(list, id, top);
+      dz[id] = Chunk<T>::pack1(empty ? 0.f : listed_grad<H>(list, id, p, x[k], top, g, tau, w, gr));
+    }
+  }
+};
+
 // First sum: the exponential at the temperature; second: the hard term's.
 template <int H>
 struct DistillTerm {
@@ -826,15 +855,18 @@ __global__ __launch_bounds__(NT) void lora_distill_fwd_kernel(const T* __restric
 }
 
 // The gradient from what the forward saved: workgroups of kGradThreads x
-// kGradKeep chunks of a row.  Bound by HBM: 4096 x 32000 bf16 in 106 us, 301 x
-// 131071 fp32 in 66, 4.8 to 5.0 TB/s read and written.
+// kGradKeep chunks of a row.  Bound by HBM: 4096 x 32000 bf16 with a list of 64 in
+// 107 us, 301 x 131071 fp32 in 60, 4.9 to 5.3 TB/s read and written (116 and 66
+// with the listed columns' logits looked up once the list was made).  Registers
+// for seven waves a SIMD: eight spill two.
 template <typename T, int H>
-__global__ __launch_bounds__(kGradThreads, 8) void lora_distill_bwd_kernel(
+__global__ __launch_bounds__(kGradThreads, 7) void lora_distill_bwd_kernel(
     const T* logits, int64_t ld, const int32_t* __restrict__ ids, const float* __restrict__ teacher,
     const int32_t* __restrict__ labels, float tau, float w, const float4* __restrict__ saved,
     const float* __restrict__ dloss, T* dlogits, int vocab, int top, int parts) {
   constexpr int CH = Chunk<T>::CH, NT = kGradThreads;
   __shared__ ListShared list;
+  __shared__ ListChain<NT> chain;
   const int64_t r = blockIdx.x / (unsigned)parts;
   const int part = (int)(blockIdx.x - (unsigned)r * (unsigned)parts), tid = threadIdx.x;
   const T* z = logits + r * ld;
@@ -846,12 +878,18 @@ __global__ __launch_bounds__(kGradThreads, 8) void lora_distill_bwd_kernel(
   const bool last = part == parts - 1;
   const int c0 = min(row.chunks, part * (NT * kGradKeep)), c1 = last ? row.chunks : min(row.chunks, c0 + NT * kGradKeep);
   const int col0 = part == 0 ? 0 : row.head + c0 * CH, col1 = last ? vocab : row.head + c1 * CH;
+  // the entries' columns, by a thread each, ahead of the list that the first wave
+  // makes of them: their logits come with the row
+  const int mine = tid < top ? ids[r * top + tid] : (tid == top && labels ? labels[r] : -1);
   int4v v[kGradKeep];
 #pragma unroll
   for (int i = 0; i < kGradKeep; ++i) {
     const int c = c0 + tid + i * NT;
     if (c < c1) v[i] = row.at(c);
   }
+  chain.first[tid] = -1;
+  const bool fixes = mine >= col0 && mine < col1;
+  const T xl = row.raw(fixes ? mine : -1);
   int edge = row.edge(vocab);
   if (edge < col0 || edge >= col1) edge = -1;
   const float xe = row.value(edge);
@@ -860,10 +898,10 @@ __global__ __launch_bounds__(kGradThreads, 8) void lora_distill_bwd_kernel(
   const float g = dloss[r];
   __syncthreads();
   const GradRow gr = grad_row(list, top, g, tau, w, sv.x, sv.y, sv.z);
-  const int mine = tid <= top ? list.id[tid] : -1;
-  const bool fixes = mine >= col0 && mine < col1;
-  float fix = 0.f;
-  if (fixes && sv.y != __builtin_inff()) fix = listed_grad<H>(list, mine, listed_p(list, mine, top), row.value(mine), top, g, tau, w, gr);
+  if (fixes) {
+    chain.x[tid] = Chunk<T>::one(xl);
+    chain.link(tid, mine < row.head ? mine : (mine >= row.tail0 ? CH + mine - row.tail0 : ((mine - row.head) / CH - c0) % NT));
+  }
   __syncthreads();   // the listed columns are read: dlogits may be the logits
 #pragma unroll
   for (int i = 0; i < kGradKeep; ++i) {
@@ -877,8 +915,7 @@ __global__ __launch_bounds__(kGradThreads, 8) void lora_distill_bwd_kernel(
     __builtin_amdgcn_sched_barrier(0);   // one chunk's values at a time
   }
   if (edge >= 0) dz[edge] = Chunk<T>::pack1(gr.template dense<H>(xe));
-  __syncthreads();   // the listed columns over the dense values
-  if (fixes) dz[mine] = Chunk<T>::pack1(fix);
+  chain.template put<H>(dz, list, top, sv.y == __builtin_inff(), g, tau, w, gr);
 }
 
 // Loss and gradient in one pass over the logits.  A workgroup keeps a row in
@@ -896,9 +933,7 @@ __global__ __launch_bounds__(kGradThreads, 8) void lora_distill_bwd_kernel(
 template <int NT>
 struct StepShared {
   ListShared list;
-  float x[kMaxTop + 1];         // the entries' logits
-  int next[kMaxTop + 1];        // chain of a thread's entries, -1: end
-  int first[NT];
+  ListChain<NT> chain;
   float mbox[NT / 64];
   float2 sbox[NT / 64];
 };
@@ -943,7 +978,7 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     StepShared<NT>& sh = both[turn];
     T* dz = dlogits + r * ld;
     if (tid < 64) teacher_list(in, kLog2e / tau, vocab, top, sh.list);
-    sh.first[tid] = -1;
+    sh.chain.first[tid] = -1;
     const float xe = Chunk<T>::one(xe_in);
     float m = xe;
 #pragma unroll
@@ -960,7 +995,7 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     const T xl = row.raw(mine);
     if (mine >= 0) {
       const int owner = mine < row.head ? mine : (mine >= row.tail0 ? CH + mine - row.tail0 : (mine - row.head) / CH % NT);
-      sh.next[tid] = atomicExch(&sh.first[owner], tid);
+      sh.chain.link(tid, owner);
     }
     // the next row
     const int64_t rn = r + gridDim.x;
@@ -992,7 +1027,7 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     }
     add(xe);
     if constexpr (H == HARD_SAME) hard = soft;
-    if (mine >= 0) sh.x[tid] = Chunk<T>::one(xl);   // (from here on dlogits may be written over the logits)
+    if (mine >= 0) sh.chain.x[tid] = Chunk<T>::one(xl);   // (from here on dlogits may be written over the logits)
     const float2 sum = block_sum2<NT>(soft, hard, sh.sbox);
     const bool empty = sum.x == 0.f;
     const float inf = __builtin_inff();
@@ -1031,20 +1066,9 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
     }
     const int edge = row.edge(vocab);
     if (edge >= 0) dz[edge] = Chunk<T>::pack1(gr.template dense<H>(xe));
-    for (int k = sh.first[tid]; k >= 0; k = sh.next[k]) {
-      const int id = sh.list.id[k];
-      float p = 0.f;      // (the sum of two is the same in either order, the list has that of more)
-      int same = 0;
-      for (int j = sh.first[tid]; j >= 0; j = sh.next[j])
-        if (sh.list.id[j] == id) {
-          p += sh.list.p[j];
-          ++same;
-        }
-      if (same > 2) p = listed_p(sh.list, id, top);
-      dz[id] = Chunk<T>::pack1(empty ? 0.f : listed_grad<H>(sh.list, id, p, sh.x[k], top, g, tau, w, gr));
-    }
+    sh.chain.template put<H>(dz, sh.list, top, empty, g, tau, w, gr);
     if (tid < 64) {
-      const float l = row_loss(sh.list, [&](int k) LORA_INLINE { return sh.x[k]; }, top, tau, w, shift, logf(sum.x), logf(sum.y));
+      const float l = row_loss(sh.list, [&](int k) LORA_INLINE { return sh.chain.x[k]; }, top, tau, w, shift, logf(sum.x), logf(sum.y));
       if (tid == 0) loss[r] = empty ? 0.f : l;
     }
     if (!more) break;
@@ -1069,12 +1093,14 @@ __global__ __launch_bounds__(NT) void lora_distill_wide_kernel(const T* logits, 
                                                                int top) {
   constexpr int CH = Chunk<T>::CH, U = 8;
   __shared__ ListShared list;
+  __shared__ ListChain<NT> chain;
   __shared__ Unit box[kMaxUnits];
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x;
   T* dz = dlogits + r * ld;
   const bool alike = lies_alike<T>(logits, dlogits);
   const Row<T> row(logits + r * ld, vocab);
+  chain.first[tid] = -1;
   const float g = dloss[r];
   if (tid < 64) teacher_list(list_in(ids + r * top, teacher + r * top, labels ? labels + r : nullptr, top), kLog2e / tau, vocab, top, list);
   const int edge = row.edge(vocab);
@@ -1090,8 +1116,10 @@ __global__ __launch_bounds__(NT) void lora_distill_wide_kernel(const T* logits, 
     }
     const GradRow gr = grad_row(list, top, g, tau, w, shift, empty ? inf : sum.s, empty ? inf : sum.a);
     const int mine = tid <= top ? list.id[tid] : -1;
-    float fix = 0.f;
-    if (mine >= 0 && !empty) fix = listed_grad<H>(list, mine, listed_p(list, mine, top), row.value(mine), top, g, tau, w, gr);
+    if (mine >= 0) {
+      chain.x[tid] = row.value(mine);
+      chain.link(tid, mine < row.head ? mine : (mine >= row.tail0 ? CH + mine - row.tail0 : (mine - row.head) / CH % NT));
+    }
     __syncthreads();   // the listed columns are read: dlogits may be the logits
     for (int c0 = tid; c0 < row.chunks; c0 += NT * U) {
       int4v v[U];
@@ -1108,8 +1136,7 @@ __global__ __launch_bounds__(NT) void lora_distill_wide_kernel(const T* logits, 
         }
     }
     if (edge >= 0) dz[edge] = Chunk<T>::pack1(gr.template dense<H>(xe));
-    __syncthreads();   // the listed columns over the dense values
-    if (mine >= 0) dz[mine] = Chunk<T>::pack1(fix);
+    chain.template put<H>(dz, list, top, empty, g, tau, w, gr);
   });
 }
 
