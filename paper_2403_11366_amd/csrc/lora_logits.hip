@@ -822,8 +822,9 @@ __device__ __forceinline__ Unit row_sums(const Row<T>& row, float xe, float scal
 }
 
 // The loss of every row, and what the gradient needs.  Bound by HBM: 4096 x 32000
-// bf16 in 49 us, 5.4 TB/s; 301 x 131071 fp32 in 36, 4.4 TB/s (301 workgroups on
-// 256 compute units).
+// bf16 in 49 us, 5.4 TB/s; 301 x 131071 fp32 in 36 to 40, 4.0 to 4.4 TB/s (301
+// workgroups on 256 compute units).  A unit's loads ahead of the last one's sums
+// were slower (53 us): other waves cover the loads.
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void lora_distill_fwd_kernel(const T* __restrict__ logits, int64_t ld,
                                                               const int32_t* __restrict__ ids,
