@@ -928,7 +928,7 @@ __global__ __launch_bounds__(kGradThreads, 7) void lora_distill_bwd_kernel(
 // chain of entries per thread in LDS), in its program order, so no barrier waits
 // for the stores; two LDS copies alternate, so that none waits for the row's end.
 // Chunks are loaded and stored through buffer resources of the row's whole
-// chunks: those past it are not stored.  Bound by HBM: 4096 x 32000 bf16 with a
+// chunks: those past it are neither read nor stored.  Bound by HBM: 4096 x 32000 bf16 with a
 // list of 64 in 99 us, 5.3 TB/s, a copy's rate (124 with the exponentials formed
 // again and the loads behind the stores).
 template <int NT>
@@ -962,7 +962,8 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
   int4v v[KEEP];
   __amdgpu_buffer_rsrc_t rs = make_rsrc(uniform_ptr(row.p + row.head), (uint64_t)uniform(row.chunks) * 16);
   auto load = [&](int i) LORA_INLINE {
-    return __builtin_bit_cast(int4v, __builtin_amdgcn_raw_buffer_load_b128(rs, tid * 16, i * NT * 16, 0));
+    // (the whole offset in the lane's register, where it is compared with the row's size)
+    return __builtin_bit_cast(int4v, __builtin_amdgcn_raw_buffer_load_b128(rs, (tid + i * NT) * 16, 0, 0));
   };
   auto past = [&](int i, int chunks) LORA_INLINE {   // -inf in the chunks past the row
     if ((i + 1) * NT > chunks)
