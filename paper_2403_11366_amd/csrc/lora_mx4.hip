@@ -381,7 +381,6 @@ __global__ __launch_bounds__(64 * WM * WN) void lora_mx4_kernel(
   const uint32_t rowbytes = (uint32_t)slabs * 128;
   const __amdgpu_buffer_rsrc_t rsX = make_rsrc(Xc + (size_t)m0 * rowbytes, (uint64_t)min(BM, m - m0) * rowbytes);
   const __amdgpu_buffer_rsrc_t rsW = make_rsrc(Wc + (size_t)n0 * rowbytes, (uint64_t)min(BN, n - n0) * rowbytes);
-  // (cells past the matrix: another's, or zeros past the end)
   const int gx = (m + 63) / 64, gw = (n + 63) / 64;
   const __amdgpu_buffer_rsrc_t rsXs = make_rsrc(Xs, (uint64_t)gx * slabs * 512);
   const __amdgpu_buffer_rsrc_t rsWs = make_rsrc(Ws, (uint64_t)gw * slabs * 512);
@@ -399,28 +398,29 @@ __global__ __launch_bounds__(64 * WM * WN) void lora_mx4_kernel(
   const uint32_t coff = (uint32_t)(crow + l8) * rowbytes + kcol;
   // the wave's half cells (uniform): their matrix, first cell and cells per slab
   __amdgpu_buffer_rsrc_t rsS[CS + 1];
-  uint32_t sat[CS + 1], sstep[CS + 1], slane[CS + 1];
+  uint32_t sat[CS + 1], sstep[CS + 1], slane[CS + 1];   // (a cell past the matrix: zeros)
 #pragma unroll
   for (int i = 0; i < CS; ++i) {
     const int h = wave * CS + i, cl = h >> 1;
     const bool isx = cl < XCELLS;
     rsS[i] = isx ? rsXs : rsWs;
-    sat[i] = (uint32_t)(isx ? m0 / 64 + cl : n0 / 64 + cl - XCELLS) * 512 + (h & 1) * 256;
-    sstep[i] = (uint32_t)(isx ? gx : gw) * 512;
-    slane[i] = cl < CELLS ? (uint32_t)lane * 4 : kOOB;
+    const Mx4Cell at = cl < CELLS ? mx4_cell(isx ? m0 / 64 + cl : n0 / 64 + cl - XCELLS, isx ? gx : gw) : Mx4Cell{0u, 0u, kMx4None};
+    sat[i] = at.first + (h & 1) * 256;
+    sstep[i] = at.step;
+    slane[i] = (uint32_t)lane * 4 | at.none;
   }
-  // copy i of slab kb into the stage at `stage`; past the last slab (past = kOOB,
-  // else 0) zeros, so that the counts below hold
-  auto copy = [&](int kb, int i, int stage, uint32_t past) LORA_INLINE {
+  // copy i of a slab into the stage at `stage`; past the last slab zeros, so that
+  // the counts below hold
+  auto copy = [&](const Mx4Slab& s, int i, int stage) LORA_INLINE {
     char* sb = smem + stage;
     if (i < CX) {
-      dma16(rsX, (coff + (uint32_t)(8 * NW * i) * rowbytes) | past, (uint32_t)kb * 128, sb + (crow + 8 * NW * i) * 128);
+      dma16(rsX, (coff + (uint32_t)(8 * NW * i) * rowbytes) | s.none, s.kb * 128, sb + (crow + 8 * NW * i) * 128);
     } else if (i < CX + CW) {
       const int r = 8 * NW * (i - CX);
-      dma16(rsW, (coff + (uint32_t)r * rowbytes) | past, (uint32_t)kb * 128, sb + (BM + crow + r) * 128);
+      dma16(rsW, (coff + (uint32_t)r * rowbytes) | s.none, s.kb * 128, sb + (BM + crow + r) * 128);
     } else {
       const int c = i - CX - CW;
-      dma4(rsS[c], slane[c] | past, sat[c] + (uint32_t)kb * sstep[c], sb + SOFF + (wave * CS + c) * 256);
+      dma4(rsS[c], slane[c] | s.none, sat[c] + s.kb * sstep[c], sb + SOFF + (wave * CS + c) * 256);
     }
   };
   const uint32_t fbase = kc_offset(c16, g);      // (rows 16 apart swizzle alike; step 1: chunk 4 further)
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(64 * WM * WN) void lora_mx4_kernel(
     for (int i = 0; i < SX; ++i) sx1[i] = *reinterpret_cast<const int2v*>(sc + (wm * SX + i) * 512);
     sw1 = *reinterpret_cast<const int2v*>(sc + (XCELLS + wn) * 512);
   };
-  auto load_scales = [&](int kb) LORA_INLINE {   // SL loads, in this place
+  auto load_scales = [&](int kb) LORA_INLINE {   // SL loads, in this place (cells past the matrix: another's, or zeros past the end)
     const uint32_t cx = (uint32_t)kb * gx + m0 / 64 + SX * wm, cw = (uint32_t)kb * gw + n0 / 64 + wn;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(64 * WM * WN) void lora_mx4_kernel(
 #pragma unroll
   for (int j = 0; j < NS; ++j)
 #pragma unroll
-    for (int i = 0; i < C; ++i) copy(j, i, j * STAGE, j < slabs ? 0u : kOOB);
+    for (int i = 0; i < C; ++i) copy(mx4_slab(j, slabs), i, j * STAGE);
   copy_barrier<(NS - 1) * C>();
   int here = 0;
   if constexpr (!SREG) read_scales(here);
@@ -493,11 +493,11 @@ __global__ __launch_bounds__(64 * WM * WN) void lora_mx4_kernel(
     copy_barrier<(NS - 2) * C + SL>();   // every wave has read this slab, and the next one has landed
     if constexpr (!SREG) read_scales(there);
     read_w(there, 0);
-    const uint32_t past = kb + NS < slabs ? 0u : kOOB;
+    const Mx4Slab later = mx4_slab(kb + NS, slabs);
     products(I1{}, [&](int b) LORA_INLINE {
 #pragma unroll
       for (int i = 0; i < CPB; ++i)
-        if (CPB * b + i < C) copy(kb + NS, CPB * b + i, here, past);
+        if (CPB * b + i < C) copy(later, CPB * b + i, here);
       read_x(there, 0, b);
     });
     here = there;

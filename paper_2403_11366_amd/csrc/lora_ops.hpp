@@ -233,6 +233,24 @@ inline Mx4Plan plan_mx4_fwd(int64_t m, int64_t n, int64_t k) {
   return best;
 }
 
+// What a tile's copies read.  A copy's address is a scalar offset, the same for
+// the wave, and a lane offset.  The lanes' alone is sure to be compared with the
+// operand's size, or with that size less the scalar offset: what lies past the
+// operand has a lane offset past any operand and a scalar offset inside it.
+constexpr uint32_t kMx4None = 0x80000000u;
+struct Mx4Slab {
+  uint32_t kb, none;           // the slab of the scalar offset; kMx4None or 0, for the lanes
+};
+__host__ __device__ inline Mx4Slab mx4_slab(int kb, int slabs) {
+  return kb < slabs ? Mx4Slab{(uint32_t)kb, 0u} : Mx4Slab{0u, kMx4None};
+}
+struct Mx4Cell {
+  uint32_t first, step, none;  // byte of a cell of scales in slab 0, bytes from slab to slab; as above
+};
+__host__ __device__ inline Mx4Cell mx4_cell(int cell, int cells) {
+  return cell < cells ? Mx4Cell{(uint32_t)cell * 512, (uint32_t)cells * 512, 0u} : Mx4Cell{0u, 0u, kMx4None};
+}
+
 // Workspace of the 4-bit forward: X's codes and scales.
 struct Mx4Layout {
   size_t xc, xs, total;
