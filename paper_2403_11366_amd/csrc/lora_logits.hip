@@ -665,24 +665,26 @@ __device__ __forceinline__ void teacher_list(ListIn in, float scale, int vocab, 
 }
 
 // Loss of a row by one wave from the logarithms of both softmaxes' sums; x(k) is
-// entry k's logit.
+// entry k's logit.  The soft term's sum is taken over z - max z, before the
+// temperature: divided by one below 1, the type's lowest value (a banned column
+// that the teacher lists) would pass fp32's range where the loss does not.
 template <typename X>
 __device__ __forceinline__ float row_loss(const ListShared& sh, X&& x, int top, float tau, float w, float shift,
                                           float lnsoft, float lnhard) {
   const int lane = threadIdx.x & 63;
-  const float itau = 1.f / tau;
-  float cross = 0.f;       // sum p ln q
+  float cross = 0.f;       // sum p (z - max z)
   if (w > 0.f)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int k = lane + 64 * h;
       if (k < top && sh.id[k] >= 0) {
         const float p = sh.p[k];
-        if (!(p == 0.f)) cross = fmaf(p, (x(k) - shift) * itau - lnsoft, cross);
+        if (!(p == 0.f)) cross = fmaf(p, x(k) - shift, cross);
       }
     }
   cross = wave_sum(cross);
-  float loss = w > 0.f ? w * tau * tau * (sh.entropy - cross) : 0.f;
+  // (without entries: no soft term, whatever the row's sum)
+  float loss = w > 0.f && sh.mass != 0.f ? w * tau * (tau * fmaf(sh.mass, lnsoft, sh.entropy) - cross) : 0.f;
   if (w < 1.f && sh.id[top] >= 0)
     loss += (1.f - w) * (lnhard - (x(top) - shift));
   return loss;
