@@ -389,7 +389,7 @@ typedef enum { LORA_BF16 = 0, LORA_F32 = 1 } lora_dtype;
  *            i at element i ld, ld >= vocab (any), read only
  *   tokens   [rows], or NULL with logp NULL.  A token outside [0, vocab) is
  *            none: its logp is 0
- *   temperature  above 0 and finite (else LORA_ERR_SHAPE)
+ *   temperature  from 2^-126 and finite (else LORA_ERR_SHAPE)
  *   logp, entropy  [rows] fp32, written
  *   top      alternatives per row, 0 .. min(vocab, 128) (above vocab
  *            LORA_ERR_SHAPE, above 128 LORA_ERR_UNSUPPORTED); 0 leaves top_ids
@@ -431,7 +431,7 @@ lora_status lora_token_logprobs(const void* logits, lora_dtype dtype, int64_t ld
  *            than top); entries of one id add up
  *   labels   [rows], or NULL with soft_weight 1.  A label outside [0, vocab) is
  *            none
- *   temperature  above 0 and finite; soft_weight in [0, 1] (else LORA_ERR_SHAPE)
+ *   temperature  from 2^-63 to 2^63; soft_weight in [0, 1] (else LORA_ERR_SHAPE)
  *   loss     [rows] fp32, written
  *   saved    [rows, 4] fp32: written by the forward for the backward
  *   dloss    [rows] fp32, read only

@@ -16,6 +16,11 @@ constexpr int64_t kMaxElems = int64_t(1) << 30;     // any one matrix of theirs 
 constexpr int64_t kMaxRows = int64_t(1) << 21;      // rows of logits
 constexpr int64_t kMaxVocab = int64_t(1) << 20;     // their columns
 constexpr int64_t kMaxLogits = int64_t(1) << 34;    // rows x row pitch
+// Temperatures: 1/T and log2(e)/T are finite from the smallest normal number on (an
+// infinite one times a row's maximum less itself is NaN); the distillation's T^2
+// and its inverse are normal numbers between these two.
+constexpr float kMinTemperature = 0x1p-126f;
+constexpr float kMinDistillTemperature = 0x1p-63f, kMaxDistillTemperature = 0x1p63f;
 
 struct Range {
   uintptr_t lo, hi;  // [lo, hi)
@@ -96,7 +101,7 @@ lora_status check_distill(const void* logits, int dtype, int64_t ld, const int32
   if (st != LORA_OK) return st;
   if (top < 1) return LORA_ERR_SHAPE;
   if (top > lora::kMaxTop) return LORA_ERR_UNSUPPORTED;
-  if (!(tau > 0.0f && tau < INFINITY) || !(w >= 0.0f && w <= 1.0f)) return LORA_ERR_SHAPE;
+  if (!(tau >= kMinDistillTemperature && tau <= kMaxDistillTemperature) || !(w >= 0.0f && w <= 1.0f)) return LORA_ERR_SHAPE;
   if (!labels && w != 1.0f) return LORA_ERR_NULL;
   if (!aligned(logits, elem_bytes(dtype)) || !aligned4(ids) || !aligned4(teacher) || !aligned4(labels))
     return LORA_ERR_ALIGN;
@@ -198,7 +203,7 @@ lora_status lora_token_logprobs(const void* logits, lora_dtype type, int64_t ld,
   const lora_status st = check_logits(rows, vocab, ld, top);
   if (st != LORA_OK) return st;
   if (top > 0 && (!top_ids || !top_logp)) return LORA_ERR_NULL;
-  if (!(temperature > 0.0f && temperature < INFINITY)) return LORA_ERR_SHAPE;
+  if (!(temperature >= kMinTemperature && temperature < INFINITY)) return LORA_ERR_SHAPE;
   if (!aligned(logits, elem_bytes(dtype)) || !aligned4(tokens) || !aligned4(logp) || !aligned4(entropy) ||
       (top > 0 && (!aligned4(top_ids) || !aligned4(top_logp))))
     return LORA_ERR_ALIGN;
