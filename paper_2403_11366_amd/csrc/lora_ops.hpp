@@ -198,10 +198,13 @@ inline Mx4Plan mx4_plan_of(Mx4Kind kind, int64_t m, int64_t n, int bm, int bn, i
 inline Mx4Plan plan_mx4_fwd(int64_t m, int64_t n, int64_t k) {
   const int64_t slabs = mx4_slabs(k), groups = (n + 15) / 16;
   if (m <= kTokenRows && m * k <= (1 << 15) && mx4_token_lds(slabs) <= 160 * 1024) {
-    // eight waves share a group of 16 features while that leaves no compute unit a
-    // second round, else two (1 x 32000 x 4096 14 us, 17 with eight; 1 x 4096 x 4096
-    // 7.3, 4.7 with eight)
-    const bool eight = groups <= 384;
+    // eight waves share a group of 16 features up to 512 groups, of more than eight
+    // tokens (which each workgroup quantises) up to 256, else two.  Eight and two, us:
+    // 1 x 4096 x 4096 4.5, 7.0; 1 x 8192 x 4096 5.8, 7.2; 1 x 16384 x 4096 10.8, 9.1;
+    // 1 x 4096 x 13824 (one workgroup to a compute unit's LDS) 8.7, 18.0; 1 x 8192 x
+    // 13824 17.5, 20.5; 1 x 11008 x 13824 24.0, 21.5; 8 x 8192 x 4096 9.2, 9.0; 16 x
+    // 4096 x 2048 5.7, 6.7; 16 x 5120 x 2048 7.8, 6.7
+    const bool eight = groups <= (m <= 8 ? 512 : 256);
     return mx4_plan_of(eight ? MX4_TOKEN_8 : MX4_TOKEN_2, 1, n, 1, eight ? 16 : 64, 512);
   }
   Mx4Plan best{};

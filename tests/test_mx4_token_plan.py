@@ -21,3 +21,11 @@ def test_gpu_sizes_reach_the_widest_inputs(driver):  # noqa: F811
         assert {m for (m, n, k), q in of.items() if q == kind and k > 8448} >= {1, 2, 3}
     # ragged against the 16 features of a group and the 64 of a cell of scales
     assert any(n % 16 for m, n, k in of) and any(n % 64 and n % 16 == 0 for m, n, k in of)
+
+
+def test_eight_waves_to_a_group_of_features(driver):  # noqa: F811
+    """Up to 512 groups, of more than eight tokens up to 256, at every width (measured on both sides)."""
+    for k in (4096, 8192, 8704, 11008, 13824, 16384):
+        sizes = [(1, 16 * groups, k) for groups in (1, 256, 320, 384, 448, 512, 513, 1024)]
+        assert kinds(driver, sizes) == [0] * 6 + [1] * 2, k
+    assert kinds(driver, [(8, 8192, 4096), (8, 8200, 4096), (16, 4096, 2048), (16, 4104, 2048), (16, 5120, 512)]) == [0, 1, 0, 1, 1]
