@@ -511,7 +511,7 @@ def lora_token_logprobs(logits, tokens, logp, entropy, top_ids, top_logp, worksp
     code, ld, rows, vocab = _check_logits(logits)
     if (tokens is None) != (logp is None) or (top_ids is None) != (top_logp is None):
         raise ValueError("tokens and logp, top_ids and top_logp: both or neither")
-    top = 0 if top_ids is None else top_ids.shape[1]
+    top = 0 if top_ids is None or top_ids.dim() != 2 else top_ids.shape[1]
     _check_rows((entropy, "entropy", _F32, (rows,)))
     if tokens is not None:
         _check_rows((tokens, "tokens", _I32, (rows,)), (logp, "logp", _F32, (rows,)))
