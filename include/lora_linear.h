@@ -341,9 +341,9 @@ lora_status lora_linear_group_bwd(const lora_bf16* const* dY, const lora_bf16* X
  *           lane of a matrix product so finds the scales of four rows 16 apart
  *           and two blocks 4 apart in 8 bytes.  Zero for the rows and blocks
  *           of a cell beyond the matrix.
- * rows >= 1, k >= 8 and a multiple of 8 (LORA_ERR_SHAPE), rows x 256
- * ceil(k/256) at most 2^30 (LORA_ERR_UNSUPPORTED).  The sizes are in bytes, 0 on
- * invalid arguments.
+ * rows >= 1, k >= 8 and a multiple of 8 (LORA_ERR_SHAPE), rows and k at most 2^22,
+ * rows x 256 ceil(k/256) at most 2^30 (LORA_ERR_UNSUPPORTED).  The sizes are in
+ * bytes, 0 on invalid arguments.
  */
 size_t lora_mx4_codes_size(int64_t rows, int64_t k);
 size_t lora_mx4_scales_size(int64_t rows, int64_t k);
@@ -352,7 +352,8 @@ size_t lora_mx4_scales_size(int64_t rows, int64_t k);
 lora_status lora_mx4_quantize(const lora_bf16* X, uint8_t* codes, uint8_t* scales, int64_t rows, int64_t k,
                               void* stream);
 
-/* The values that codes and scales stand for, X [rows, k] (bf16, exact). */
+/* The values that codes and scales stand for, X [rows, k] (bf16, exact; scales of 253
+ * and 254, which lora_mx4_quantize does not write, pass its range to infinity). */
 lora_status lora_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, lora_bf16* X, int64_t rows, int64_t k,
                                 void* stream);
 
@@ -367,8 +368,8 @@ lora_status lora_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, lor
  *   Y         [m, n] bf16, written
  *   workspace at least lora_linear_mx4_fwd_workspace_size(m, n, k) bytes (0 on
  *             an invalid shape), 16-byte aligned, not used concurrently
- * A block of X or W with a NaN or an infinity makes every output that it enters
- * NaN.
+ * The rules above apply to X and W, m n is at most 2^30.  A block of X or W with a
+ * NaN or an infinity makes every output that it enters NaN.
  */
 size_t lora_linear_mx4_fwd_workspace_size(int64_t m, int64_t n, int64_t k);
 lora_status lora_linear_mx4_fwd(const lora_bf16* X, const uint8_t* W_codes, const uint8_t* W_scales, lora_bf16* Y,
@@ -414,7 +415,8 @@ lora_status lora_token_logprobs(const void* logits, lora_dtype dtype, int64_t ld
 /*
  * Distillation from a teacher's top logits.  Row i of the teacher's lists holds
  * ids id_k and logits t_k, k < top (for instance the top_ids and top_logp of
- * lora_token_logprobs: adding a number to a row's t changes nothing).  With p =
+ * lora_token_logprobs at temperature 1: adding a number to a row's t changes
+ * nothing, a factor does).  With p =
  * softmax(t / T) over the entries whose id lies in [0, vocab), q = softmax(z /
  * T) over the whole vocabulary, T the temperature and w the soft weight,
  *

@@ -241,21 +241,25 @@ __device__ __forceinline__ Unit join_units(const Unit* box, int n, const Term& t
 // of the threads' own maxima is at most the top-th largest value, so only the
 // few threads whose maximum reaches it (the owners) hold values to look at.  A
 // lower bound of it comes from one wave's bisection over maxima of groups of threads.  The
-// owners' chunks are read again, sixteen lanes an owner; the values at or above
+// owners' chunks are read again, four lanes an owner; the values at or above
 // the bound go into an LDS list and are ranked against each other by value and
-// index.  Where more values tie than the list holds (a constant row), the exact
-// top-th value is found by counting over the row, four bits a pass, and its
-// lowest columns by counting on from the row's start.
+// index.  Where more values tie than the list holds (a constant row, or one with
+// fewer than `top` values above -inf, where -inf ties), the exact top-th value is
+// found by counting over the row, four bits a pass, and its lowest columns by
+// counting on from the row's start: 6 passes over a bf16 row and 10 over an fp32
+// one, an element a load.
 //
 // Few rows of many units are split over workgroups: each leaves its units and
 // its own top values in the workspace, and a second launch joins them.
 //
 // Bound by HBM, and by the selection's latency at a row's end where few other rows
-// cover it: 4096 x 32000 bf16 53 us (5.0 TB/s) without alternatives, 60 with 20;
-// 777 x 50021 fp32 34 and, with 64, 44; one row of 32000 4.4 and, with 20, 7.8;
-// one of 131072 fp32 with 20, split, 12 (25 in one workgroup).  Reading all
-// chunks of an owning thread again, instead of one unit's, fetched more lines
-// than the row has (777 x 50021: 52).
+// cover it: 4096 x 32000 bf16 55 us (4.7 TB/s) without alternatives, 60 with 20;
+// 777 x 50021 fp32 33 and, with 64, 41; one row of 32000 4.0 and, with 20, 7.4;
+// one of 131072 fp32 with 20, split, 7.6 and 4.6 to join (17 in one workgroup).
+// Reading all chunks of an owning thread again, instead of one unit's, fetched
+// more lines than the row has (777 x 50021: 52).  By counting, with ten columns
+// above -inf: 4096 x 32000 837 us, 777 x 50021 755, one row of 32000 89, one of
+// 131072 fp32 110 and 5; constant rows take as long.
 
 struct EntropyTerm {
   float scale;   // log2(e) / tau
@@ -693,7 +697,7 @@ __device__ __forceinline__ float row_loss(const ListShared& sh, X&& x, int top, 
 // How the two softmaxes' exponentials of an element are formed from u = 2^((z -
 // max z) scale): one where the temperature is 1 or a term has no weight, a power
 // of u at temperatures 2 and 4, else an exponential of its own (4096 x 32000
-// bf16: the step takes 98 us at temperatures 1, 2 and 4, 134 at 3).
+// bf16: the step takes 99 to 101 us at temperatures 1, 2 and 4, 137 at 3).
 enum Hard { HARD_SAME, HARD_SQUARE, HARD_FOURTH, HARD_OWN };
 __host__ __device__ __forceinline__ Hard hard_of(float tau, float w) {
   if (tau == 1.f || w == 1.f || w == 0.f) return HARD_SAME;
@@ -824,9 +828,10 @@ __device__ __forceinline__ Unit row_sums(const Row<T>& row, float xe, float scal
 }
 
 // The loss of every row, and what the gradient needs.  Bound by HBM: 4096 x 32000
-// bf16 in 49 us, 5.4 TB/s; 301 x 131071 fp32 in 36 to 40, 4.0 to 4.4 TB/s (301
-// workgroups on 256 compute units).  A unit's loads ahead of the last one's sums
-// were slower (53 us): other waves cover the loads.
+// bf16 in 50 us, 5.2 TB/s; 301 x 131071 fp32 in 34, 4.6 TB/s (301 workgroups on 256
+// compute units); 75 and 49 right behind a gradient that is still on its way to
+// memory.  A unit's loads ahead of the last one's sums were slower (53 us, 49
+// without in the same run): other waves cover the loads.
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void lora_distill_fwd_kernel(const T* __restrict__ logits, int64_t ld,
                                                               const int32_t* __restrict__ ids,
@@ -859,9 +864,10 @@ __global__ __launch_bounds__(NT) void lora_distill_fwd_kernel(const T* __restric
 
 // The gradient from what the forward saved: workgroups of kGradThreads x
 // kGradKeep chunks of a row.  Bound by HBM: 4096 x 32000 bf16 with a list of 64 in
-// 107 us, 301 x 131071 fp32 in 60, 4.9 to 5.3 TB/s read and written (116 and 66
-// with the listed columns' logits looked up once the list was made).  Registers
-// for seven waves a SIMD: eight spill two.
+// 103 us, 301 x 131071 fp32 in 60, 5.1 to 5.3 TB/s read and written, run after run;
+// 86 and 51 right behind the forward, with logits still in the caches (116 and 66,
+// against 107 and 60 in the same run, with the listed columns' logits looked up
+// once the list was made).  Registers for seven waves a SIMD: eight spill two.
 template <typename T, int H>
 __global__ __launch_bounds__(kGradThreads, 7) void lora_distill_bwd_kernel(
     const T* logits, int64_t ld, const int32_t* __restrict__ ids, const float* __restrict__ teacher,
@@ -1085,7 +1091,7 @@ __global__ __launch_bounds__(NT) void lora_distill_step_kernel(const T* logits, 
 }
 
 // Rows wider than a workgroup's registers: the row is read again for the gradient
-// (301 x 131071 fp32 119 us; its passes follow each other in a workgroup, so it
+// (301 x 131071 fp32 120 us; its passes follow each other in a workgroup, so it
 // takes what the forward and the backward take together or somewhat more).
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void lora_distill_wide_kernel(const T* logits, int64_t ld,

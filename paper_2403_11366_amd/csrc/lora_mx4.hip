@@ -62,8 +62,9 @@ __device__ __forceinline__ uint32_t quantise_piece(const int4v& x, int& scale) {
 // Quantisation.  A workgroup takes 16 rows x 256 columns, a quarter of a cell of
 // scales: four rows and those 16, 32 and 48 after them, whose scales stand
 // together.  Four lanes a block, each 8 columns.  Reads 2 bytes and writes 0.53 a
-// column; bound by HBM: 11008 x 4096 in 21.6 us, 5.3 TB/s (30.6 with workgroups of
-// whole cells, whose 2752 leave the last third of the run half empty).
+// column; bound by HBM: 11008 x 4096 in 21 us, 5.4 TB/s, run after run (30.6 with
+// workgroups of whole cells, whose 2752 leave the last third of the run half empty);
+// 26 right behind the inverse, whose stores are still on their way to memory.
 __global__ __launch_bounds__(256) void lora_mx4_quantize_kernel(const u16* __restrict__ X, uint8_t* __restrict__ codes,
                                                                 uint8_t* __restrict__ scales, int rows, int k,
                                                                 int slabs, int groups) {
@@ -96,8 +97,8 @@ __global__ __launch_bounds__(256) void lora_mx4_quantize_kernel(const u16* __res
 }
 
 // The values of codes and scales: a lane takes 8 columns of two rows, a workgroup
-// 16 rows x 256 columns.  Bound by HBM: 11008 x 4096 in 19.1 us, 6.0 TB/s (22 with
-// 64 rows).
+// 16 rows x 256 columns.  Bound by HBM: 11008 x 4096 in 25 us, 4.5 TB/s, run after
+// run; 18 right behind the quantisation, with codes still in the caches.
 __global__ __launch_bounds__(256) void lora_mx4_dequantize_kernel(const uint8_t* __restrict__ codes,
                                                                   const uint8_t* __restrict__ scales,
                                                                   u16* __restrict__ X, int rows, int k, int slabs,
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(256) void lora_mx4_dequantize_kernel(const uint8_t*
 // waves' sums are added, in wave order, through LDS.  A lane loads the 16 bytes
 // of codes that it multiplies; each wave has the next slab's loads in flight
 // under the current one's products.  Bound by the latency of a wave's few slabs:
-// 128 x 4096 x 4096 9 us with the quantisation, 10 on 64 x 128 tiles.
+// 128 x 4096 x 4096 9.8 us, 11.4 on 64 x 128 tiles (the quantisation, 2.5, apart).
 template <int TG, int FG>
 __global__ __launch_bounds__(512) void lora_mx4_few_kernel(const uint8_t* __restrict__ Xc,
                                                            const uint8_t* __restrict__ Xs,
@@ -229,8 +230,8 @@ __global__ __launch_bounds__(512) void lora_mx4_few_kernel(const uint8_t* __rest
 // fragments that its waves multiply; its first loads of W are under way
 // meanwhile.  A group of 16 features is formed by KS waves that share its slabs,
 // four slabs' loads of W ahead; their sums are added in wave order.  Bound by
-// launch and load latency: 1 x 4096 x 4096 in 4.7 us, 1.9 TB/s of W (two launches,
-// with X quantised by one of its own: 7.5).
+// launch and load latency: 1 x 4096 x 4096 in 4.3 us, 2.1 TB/s of W (with X quantised
+// by a launch of its own 2.5 and 4.0).
 template <int KS>
 __global__ __launch_bounds__(512) void lora_mx4_token_kernel(const u16* __restrict__ X, const uint8_t* __restrict__ Wc,
                                                              const uint8_t* __restrict__ Ws, u16* __restrict__ Y, int m,
@@ -258,7 +259,9 @@ __global__ __launch_bounds__(512) void lora_mx4_token_kernel(const u16* __restri
   for (int j = 0; j < D; ++j)
     if (ks + KS * j < slabs) load(j, ks + KS * j);
 
-  // X: four lanes a block of 32 columns; tokens past m are zeros
+  // X: four lanes a block of 32 columns.  The places of tokens past m stay as they
+  // are: a token's codes and scales enter its own column of the products alone, and
+  // those columns are not stored.
   constexpr int U = 8;   // pieces of a thread whose loads are under way together
   const int pieces = slabs * 32, total = m * pieces;
   const float inv = 1.0f / (float)pieces;
@@ -318,16 +321,20 @@ __global__ __launch_bounds__(512) void lora_mx4_token_kernel(const u16* __restri
 // Tiles of BM tokens x BN features by WM x WN waves, NS slabs in LDS, copied from
 // memory straight into LDS (one 16-byte chunk a lane, the swizzle applied to the
 // global addresses).  256 x 256, eight waves of 128 x 64: two slabs; the smaller
-// ones, for outputs that do not fill the compute units with those: three, so that
-// a slab's copies have two slabs' products to land.
+// ones, for outputs that do not fill the compute units with those: three (128 x
+// 128: four), so that a slab's copies have two slabs' products or more to land.
 //
-// 256 x 256 is bound by power: 4096 x 11008 x 4096 in 97 us, 3.8 PFLOP/s, the
-// matrix cores busy 54 to 63% of the cycles at a clock of 1.8 to 2.0 GHz.  A
-// persistent form that begins the next tile under the last one's end took 104;
-// waves of a row taking turns at the products, instead of the fragments read in
-// place, 100 to 106.  256 x 128: 1531 x 4104 x 3208 in 17.6 us, one round of 198
-// workgroups, bound by its 13 serial slabs and the tile's beginning and end.
-// 64 x 128: 24 x 32000 x 4096 in 12.3 us, 5.7 TB/s, bound by HBM.
+// 256 x 256: 4096 x 11008 x 4096 in 95 to 97 us, 3.8 to 3.9 PFLOP/s, the matrix
+// cores busy 45% of the cycles at a clock of 2.0 to 2.1 GHz.  The same launch on
+// zeros, which run at the full 2.4 GHz, takes 83 us with 43% to 44% busy: the clock is
+// worth an eighth, the rest is the loop's, where a slab's LDS reads and copies (256
+// KiB, 2048 cycles at 128 bytes) are as long as its products.  A persistent form
+// that begins the next tile under the last one's end took 104; waves of a row
+// taking turns at the products, instead of the fragments read in place, 100 to 106.
+// 256 x 128: 1531 x 4104 x 3208 in 18 us, one round of 198 workgroups with 13
+// serial slabs, of which each has 1408 cycles of LDS to 1024 of products, and the
+// tile's beginning and end.  64 x 128: 24 x 32000 x 4096 in 13 to 14 us, 5.0 to 5.4
+// TB/s, bound by HBM.
 //
 // A slab is two 128-wide steps.  A wave holds a step's fragments in registers
 // and, as soon as the four products of a token fragment are issued, reads that

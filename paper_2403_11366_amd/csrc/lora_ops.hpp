@@ -26,7 +26,7 @@ struct RowShape {
 };
 
 // Four chunks a thread, with which it can hold the exponentials too, up to 1024
-// threads; then up to 16, 64 of a thread's 128 registers (512 x 131072 bf16 66 us, 81
+// threads; then up to 16, 64 of a thread's 128 registers (512 x 131072 bf16 66 us, 79
 // read twice).
 inline RowShape row_shape(int64_t vocab, int elem) {
   const int64_t chunks = (vocab * elem + 15) / 16;
@@ -45,12 +45,16 @@ constexpr int kSmallUnits = 33;      // of the rows that 256 threads take
 inline int64_t score_units(int64_t vocab, int elem) { return (vocab * elem + kUnitBytes - 1) / kUnitBytes + 1; }
 
 // Threads to a row in the calls that only read it; a row's results do not depend
-// on them.  Few rows take 1024 threads each.  Otherwise a wave is to have units
-// to load while others reduce, but not so many that few rows leave the chip empty:
-// the forward's waves more than one unit (4096 x 32000 bf16: 48 us with 512
-// threads, 54 with 256; 8192 x 8000: 41 and 32), those of the log probabilities,
-// where a row's threads wait for its selection, more than four (4096 x 32000 with 20
-// alternatives: 78 and 67; 777 x 50021 fp32 with 64: 52 and 56).
+// on them.  Up to one row a compute unit takes 1024 threads each (256 x 32000 bf16
+// with 20 alternatives: 9.6 us, 10.0 with 512 threads, 11.7 with 256; 300 rows: 15.2,
+// 12.4, 13.0).  Otherwise a wave is to have units to load while others reduce, but
+// not so many that few rows leave the chip empty: the forward's waves more than
+// one unit (4096 x 32000 bf16: 52 us with 512 threads, 55 with 256; 8192 x 8000: 40
+// and 33), those of the log probabilities, where a row's threads wait for its
+// selection, more than four (4096 x 32000 with 20 alternatives: 65 and 61).  Up to
+// three rows a compute unit the chip has room for 512 anyway (512 x 32000: log
+// probabilities 13.2 and 14.2, forward 9.8 and 10.2; 768 rows: 16.3 and 16.2, 12.3
+// and 12.1; 900: 19.8 and 18.5, 14.1 and 13.8; rows of 8000 do not tell up to there).
 inline int read_threads(int64_t rows, int64_t vocab, int elem, int least_units) {
   if (rows <= 256) return 1024;
   return rows <= 768 || score_units(vocab, elem) > std::min(8 * least_units, kSmallUnits) ? 512 : 256;
@@ -165,16 +169,17 @@ constexpr int kTokenRows = 16;
 inline size_t mx4_token_lds(int64_t slabs) { return (size_t)slabs * 2176 + 8192; }
 
 // The one launch up to 2^15 values of X: each workgroup quantises all of them
-// (8 x 4096 x 4096 7.2 us against 7.9 in two launches, 16 x 4096 x 4096 10.2
-// against 8.2; 1 x 4096 x 4096 4.7 against 7.5).
+// (8 x 4096 x 4096 6.1 us against 2.5 + 4.3 in two launches, 16 x 4096 x 4096 8.6
+// against 2.5 + 4.7; 1 x 4096 x 4096 4.3 against 2.5 + 4.0).
 //
 // The others by their estimated time in us, launches and the quantisation left
 // out.  A round of workgroups that fills the compute units takes c + full x slabs
 // and a round of few of them c + light x slabs (the card is then short of
 // neither power nor memory); the last one lies between.  Fitted to k = 512 to
-// 16384: 4096 x 4096 x 4096 36 us on 256 x 256 (58 on 256 x 128), 2048 x 4096 x
-// 4096 24 on 256 x 128 (32), 1024 x 4096 x 4096 15 on 128 x 128 (20), 512 x 4096
-// x 4096 11 on 64 x 128 (12), 128 x 4096 x 4096 9 from memory (10).
+// 16384: 4096 x 4096 x 4096 36 us on 256 x 256 (47 on 256 x 128), 2048 x 4096 x
+// 4096 23 on 256 x 128 (28 on 256 x 256 and on 128 x 128), 1024 x 4096 x 4096 15 on
+// 128 x 128 (16 on 64 x 128, 20 on 256 x 128), 512 x 4096 x 4096 12 on 64 x 128 (13
+// on 128 x 128), 128 x 4096 x 4096 9.8 from memory (11.4 on 64 x 128).
 struct Mx4Tile {
   Mx4Kind kind;
   int bm, bn, per_cu, block;
