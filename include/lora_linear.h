@@ -464,6 +464,133 @@ lora_status lora_distill_step(const void* logits, lora_dtype dtype, int64_t ld, 
                               void* stream);
 
 /*
+ * ---- Operators of a fine-tuning step ------------------------------------------
+ * Projections without an adapter held in 8 bits (forward and the gradient through
+ * them), the loss at the output layer without its logits, and dropout whose mask is
+ * not stored.  The conventions above hold for them.
+ */
+
+/*
+ * 8-bit floating point (e4m3: sign, 4 bits of exponent, 3 of fraction, no
+ * infinities, largest value 448) with a scale 2^(s - 127), s a byte, for each block
+ * of 128 columns.  block_rows says how many rows share a block's scale: 128 (a
+ * weight) or 1 (activations); another is LORA_ERR_SHAPE.  s is the smallest with
+ * which the block's largest magnitude is at most 448 2^(s - 127), at least 0; 255,
+ * which stands for NaN, where the block holds a NaN or an infinity.  An element is
+ * its value divided by the scale, rounded to nearest (ties to even).
+ *
+ *   codes   rows of 128 ceil(k/128) bytes; zero beyond column k
+ *   scales  block_rows 128: the scale of row i, block b is byte (i/128) ceil(k/128)
+ *           + b.  block_rows 1: cells of 64 bytes, one per 64 rows and block: byte
+ *           (b ceil(rows/64) + i/64) 64 + (i%16) 4 + (i/16)%4 (whole-number
+ *           quotients); a lane of a matrix product so finds the scales of four rows
+ *           16 apart in a word.  Zero for the rows of a cell beyond the matrix.
+ * rows >= 1, k >= 8 and a multiple of 8 (LORA_ERR_SHAPE), rows and k at most 2^22,
+ * rows x 128 ceil(k/128) at most 2^30 (LORA_ERR_UNSUPPORTED).  The sizes are in
+ * bytes, 0 on invalid arguments.
+ */
+size_t lora_fp8_codes_size(int64_t rows, int64_t k);
+size_t lora_fp8_scales_size(int64_t rows, int64_t k, int block_rows);
+
+/* X [rows, k] (bf16) -> codes and scales, every byte of both written. */
+lora_status lora_fp8_quantize(const lora_bf16* X, uint8_t* codes, uint8_t* scales, int64_t rows, int64_t k,
+                              int block_rows, void* stream);
+
+/* The values that codes and scales stand for, X [rows, k] (bf16: exact from 2^-126 on;
+ * scales above 246, which lora_fp8_quantize does not write, may pass its range to
+ * infinity; a code of 127 or 255 is a NaN). */
+lora_status lora_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, lora_bf16* X, int64_t rows, int64_t k,
+                                int block_rows, void* stream);
+
+/*
+ * Linear layer with a frozen 8-bit weight W [n, k] (lora_fp8_quantize with
+ * block_rows 128), the other operand quantised on the way with block_rows 1:
+ *
+ *     forward    Y  = Q(X) Q(W)^T
+ *     backward   dX = Q(dY) Q(W)       (for W frozen: no gradient of it)
+ *
+ * The products of 8-bit values and the scales are exact.  The matrix instruction adds
+ * those of 16 neighbours of the contraction with 13 bits below the largest one's power
+ * of two (what is below is cut off), and everything else in fp32.
+ *
+ *   X, dX     [m, k] bf16
+ *   W_codes, W_scales   of W [n, k], read only
+ *   Y, dY     [m, n] bf16
+ *   workspace at least lora_linear_fp8_fwd_workspace_size(m, n, k), or ..._bwd_...,
+ *             bytes (0 on an invalid shape), 16-byte aligned, not used concurrently
+ * The rules above apply to X, W and Y.  A block of an operand with a NaN or an
+ * infinity makes every output that it enters NaN.
+ */
+size_t lora_linear_fp8_fwd_workspace_size(int64_t m, int64_t n, int64_t k);
+size_t lora_linear_fp8_bwd_workspace_size(int64_t m, int64_t n, int64_t k);
+lora_status lora_linear_fp8_fwd(const lora_bf16* X, const uint8_t* W_codes, const uint8_t* W_scales, lora_bf16* Y,
+                                void* workspace, size_t workspace_bytes, int64_t m, int64_t n, int64_t k,
+                                void* stream);
+lora_status lora_linear_fp8_bwd(const lora_bf16* dY, const uint8_t* W_codes, const uint8_t* W_scales, lora_bf16* dX,
+                                void* workspace, size_t workspace_bytes, int64_t m, int64_t n, int64_t k,
+                                void* stream);
+
+/*
+ * Dropout without a stored mask: Y = residual + keep X / (1 - p), elementwise.
+ * Element e (of the tensor in row-major order) is kept iff the 16 bits that
+ * lora_dropout_keep_mask's generator draws for element e under (seed, offset) are
+ * below floor((1 - p) 2^16 + 1/2): where rows are whole multiples of 8 elements,
+ * those are the bits of that call's mask.  The call uses the counters offset ..
+ * offset + ceil(count / 16) - 1.  The gradient of X is the same call on dY without a
+ * residual; that of the residual is dY.
+ *
+ *   X, residual, Y  [count] of type `dtype` (another: LORA_ERR_UNSUPPORTED), 16-byte
+ *             aligned; residual may be NULL (none).  Y may be X or the residual
+ *             itself; any other overlap is LORA_ERR_ALIAS
+ *   count     1 .. 2^40
+ *   p         dropout rate, 0 <= p < 1 (else LORA_ERR_SHAPE)
+ * Computed in fp32 and rounded once.  What X holds in a dropped place, NaN and
+ * infinities included, does not matter.
+ */
+lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtype dtype, int64_t count, uint64_t seed,
+                         uint64_t offset, float p, void* stream);
+
+/*
+ * Cross entropy of an output layer without its logits: z = X W^T is formed tile by
+ * tile and never kept.
+ *
+ *     loss[i] = log sum_v exp(z_iv) - z_i,labels[i]
+ *     G[i][v] = dloss[i] (softmax(z_i)_v - [v = labels[i]])
+ *     dX = G W,   dW = G^T X
+ *
+ *   X         [rows, k] bf16, read only
+ *   W         [vocab, k] bf16, read only
+ *   labels    [rows].  A label outside [0, vocab) is none: the row's loss is 0 and it
+ *             has no part in the gradients (for dW its X has to be finite)
+ *   loss      [rows] fp32, written
+ *   saved     [rows, 2] fp32: written by the forward for the backward (there may be
+ *             NULL)
+ *   dloss     [rows] fp32, read only
+ *   dX, dW    [rows, k], [vocab, k] bf16, written; one of them may be NULL
+ *   workspace at least lora_linear_xent_workspace_size(rows, vocab, k, dx, dw) bytes
+ *             (0 on invalid arguments; dx, dw: whether the call writes dX, dW; both 0
+ *             for the forward; a call with fewer outputs needs no more), 16-byte
+ *             aligned, not used concurrently
+ * Logits, their exponentials and all sums are fp32; G enters its products as bf16.
+ * A row of labels with a NaN or an infinity among its logits has loss and gradients
+ * NaN.  rows >= 1, vocab >= 1, k >= 8 and a multiple of 8 (LORA_ERR_SHAPE), rows and
+ * vocab at most 2^20, k at most 2^16, rows k at most 2^30 (LORA_ERR_UNSUPPORTED).
+ *
+ * lora_linear_xent_step: loss and gradients in one call, for a dloss known
+ * beforehand; without dW it forms the logits once.
+ */
+size_t lora_linear_xent_workspace_size(int64_t rows, int64_t vocab, int64_t k, int dx, int dw);
+lora_status lora_linear_xent_fwd(const lora_bf16* X, const lora_bf16* W, const int32_t* labels, float* loss, float* saved,
+                                 void* workspace, size_t workspace_bytes, int64_t rows, int64_t vocab, int64_t k,
+                                 void* stream);
+lora_status lora_linear_xent_bwd(const lora_bf16* X, const lora_bf16* W, const int32_t* labels, const float* saved,
+                                 const float* dloss, lora_bf16* dX, lora_bf16* dW, void* workspace,
+                                 size_t workspace_bytes, int64_t rows, int64_t vocab, int64_t k, void* stream);
+lora_status lora_linear_xent_step(const lora_bf16* X, const lora_bf16* W, const int32_t* labels, const float* dloss,
+                                  float* loss, lora_bf16* dX, lora_bf16* dW, void* workspace, size_t workspace_bytes,
+                                  int64_t rows, int64_t vocab, int64_t k, void* stream);
+
+/*
  * Launch plan of a call (host only: no GPU, no HIP call, nothing enqueued).
  * Reports, in launch order, the kernels the entry point named by `op` would
  * launch for these shapes -- the same plan the entry point itself executes --

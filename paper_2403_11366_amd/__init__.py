@@ -24,6 +24,10 @@ __all__ = [
     "lora_linear_mx4_fwd", "lora_linear_mx4_fwd_workspace_size",
     "lora_token_logprobs", "lora_token_logprobs_workspace_size",
     "lora_distill_fwd", "lora_distill_bwd", "lora_distill_step",
+    "lora_fp8_codes_size", "lora_fp8_scales_size", "lora_fp8_quantize", "lora_fp8_dequantize",
+    "lora_linear_fp8_fwd", "lora_linear_fp8_fwd_workspace_size", "lora_linear_fp8_bwd",
+    "lora_linear_fp8_bwd_workspace_size", "lora_dropout", "lora_linear_xent_fwd", "lora_linear_xent_bwd",
+    "lora_linear_xent_step", "lora_linear_xent_workspace_size",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -102,7 +106,18 @@ def load_library() -> ctypes.CDLL:
             ("lora_token_logprobs", [p, i32, i64, p, f32, p, p, p, p, p, sz, i64, i64, i64, p], i32),
             ("lora_distill_fwd", [p, i32, i64, p, p, p, f32, f32, p, p, i64, i64, i64, p], i32),
             ("lora_distill_bwd", [p, i32, i64, p, p, p, f32, f32, p, p, p, i64, i64, i64, p], i32),
-            ("lora_distill_step", [p, i32, i64, p, p, p, f32, f32, p, p, p, i64, i64, i64, p], i32)):
+            ("lora_distill_step", [p, i32, i64, p, p, p, f32, f32, p, p, p, i64, i64, i64, p], i32),
+            ("lora_fp8_codes_size", [i64, i64], sz), ("lora_fp8_scales_size", [i64, i64, i32], sz),
+            ("lora_fp8_quantize", [p, p, p, i64, i64, i32, p], i32), ("lora_fp8_dequantize", [p, p, p, i64, i64, i32, p], i32),
+            ("lora_linear_fp8_fwd_workspace_size", [i64, i64, i64], sz),
+            ("lora_linear_fp8_bwd_workspace_size", [i64, i64, i64], sz),
+            ("lora_linear_fp8_fwd", [p, p, p, p, p, sz, i64, i64, i64, p], i32),
+            ("lora_linear_fp8_bwd", [p, p, p, p, p, sz, i64, i64, i64, p], i32),
+            ("lora_dropout", [p, p, p, i32, i64, u64, u64, f32, p], i32),
+            ("lora_linear_xent_workspace_size", [i64, i64, i64, i32, i32], sz),
+            ("lora_linear_xent_fwd", [p, p, p, p, p, p, sz, i64, i64, i64, p], i32),
+            ("lora_linear_xent_bwd", [p, p, p, p, p, p, p, p, sz, i64, i64, i64, p], i32),
+            ("lora_linear_xent_step", [p, p, p, p, p, p, p, p, sz, i64, i64, i64, p], i32)):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, res
     lib.lora_linear_plan.argtypes = [ctypes.c_int, i64, pn, i64, i64, i64, ctypes.POINTER(_LaunchInfo), i64]
@@ -583,6 +598,197 @@ def lora_distill_step(logits, teacher_ids, teacher_logits, labels, dloss, loss, 
                                           _ptr(dlogits), rows, vocab, top, _stream_handle(stream))
     if st != 0:
         raise LoraError(st, "lora_distill_step")
+
+
+def lora_fp8_codes_size(rows: int, k: int) -> int:
+    return int(load_library().lora_fp8_codes_size(rows, k))
+
+
+def lora_fp8_scales_size(rows: int, k: int, block_rows: int = 128) -> int:
+    return int(load_library().lora_fp8_scales_size(rows, k, block_rows))
+
+
+def _check_fp8(codes, scales, rows, k, block_rows, name=""):
+    """8-bit codes [rows, 128 ceil(k/128)] and their scales (any shape of that many bytes)."""
+    if _BF16 is None:
+        _bind_torch()
+    blocks = (k + 127) // 128
+    if not _fits(codes, _U8, (rows, 128 * blocks)):
+        _check(codes, name + "codes", _U8, (rows, 128 * blocks))
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows: 1 (activations) or 128 (a weight)")
+    count = blocks * ((rows + 63) // 64 * 64 if block_rows == 1 else (rows + 127) // 128)
+    if scales.numel() != count or not _fits(scales, _U8, scales.shape):
+        _check(scales, name + "scales", _U8, (count,))
+
+
+def lora_fp8_quantize(X, codes, scales, block_rows: int = 128, stream=None) -> None:
+    """X [rows,k] (torch.bfloat16) in 8 bits with a scale per block of 128 columns and
+    block_rows rows (128: a weight, 1: activations): codes [rows, 128 ceil(k/128)] and
+    scales (lora_fp8_scales_size(rows, k, block_rows) bytes), torch.uint8 (layout in
+    include/lora_linear.h)."""
+    if _BF16 is None:
+        _bind_torch()
+    rows, k = X.shape
+    if not _fits(X, _BF16, (rows, k)):
+        _check(X, "X", _BF16, (rows, k))
+    _check_fp8(codes, scales, rows, k, block_rows)
+    st = load_library().lora_fp8_quantize(_ptr(X), _ptr(codes), _ptr(scales), rows, k, block_rows, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_fp8_quantize")
+
+
+def lora_fp8_dequantize(codes, scales, X, block_rows: int = 128, stream=None) -> None:
+    """The values that codes and scales stand for, into X [rows,k] (torch.bfloat16)."""
+    if _BF16 is None:
+        _bind_torch()
+    rows, k = X.shape
+    if not _fits(X, _BF16, (rows, k)):
+        _check(X, "X", _BF16, (rows, k))
+    _check_fp8(codes, scales, rows, k, block_rows)
+    st = load_library().lora_fp8_dequantize(_ptr(codes), _ptr(scales), _ptr(X), rows, k, block_rows,
+                                            _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_fp8_dequantize")
+
+
+def lora_linear_fp8_fwd_workspace_size(m: int, n: int, k: int) -> int:
+    return int(load_library().lora_linear_fp8_fwd_workspace_size(m, n, k))
+
+
+def lora_linear_fp8_bwd_workspace_size(m: int, n: int, k: int) -> int:
+    return int(load_library().lora_linear_fp8_bwd_workspace_size(m, n, k))
+
+
+def lora_linear_fp8_fwd(X, W_codes, W_scales, Y, workspace, stream=None) -> None:
+    """Y = Q(X) Q(W)^T with W [n,k] in 8 bits (lora_fp8_quantize) and X quantised on the
+    way.
+
+    X [m,k], Y [m,n]: torch.bfloat16; workspace: a device tensor of at least
+    lora_linear_fp8_fwd_workspace_size(m, n, k) bytes."""
+    if _BF16 is None:
+        _bind_torch()
+    m, k = X.shape
+    n = W_codes.shape[0]
+    if not (_fits(X, _BF16, (m, k)) and _fits(Y, _BF16, (m, n))):
+        _check(X, "X", _BF16, (m, k))
+        _check(Y, "Y", _BF16, (m, n))
+    _check_fp8(W_codes, W_scales, n, k, 128, "W_")
+    ws_bytes = _workspace_bytes(workspace)
+    st = load_library().lora_linear_fp8_fwd(_ptr(X), _ptr(W_codes), _ptr(W_scales), _ptr(Y), _ptr(workspace), ws_bytes,
+                                            m, n, k, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_linear_fp8_fwd")
+
+
+def lora_linear_fp8_bwd(dY, W_codes, W_scales, dX, workspace, stream=None) -> None:
+    """dX = Q(dY) Q(W), the gradient of lora_linear_fp8_fwd's X, dY quantised on the way.
+
+    dY [m,n], dX [m,k]: torch.bfloat16; workspace: a device tensor of at least
+    lora_linear_fp8_bwd_workspace_size(m, n, k) bytes."""
+    if _BF16 is None:
+        _bind_torch()
+    m, n = dY.shape
+    k = dX.shape[1]
+    if not (_fits(dY, _BF16, (m, n)) and _fits(dX, _BF16, (m, k))):
+        _check(dY, "dY", _BF16, (m, n))
+        _check(dX, "dX", _BF16, (m, k))
+    _check_fp8(W_codes, W_scales, n, k, 128, "W_")
+    ws_bytes = _workspace_bytes(workspace)
+    st = load_library().lora_linear_fp8_bwd(_ptr(dY), _ptr(W_codes), _ptr(W_scales), _ptr(dX), _ptr(workspace), ws_bytes,
+                                            m, n, k, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_linear_fp8_bwd")
+
+
+def lora_dropout(X, Y, seed: int, offset: int, p: float, residual=None, stream=None) -> None:
+    """Y = residual + keep X / (1 - p), keep drawn from (seed, offset) wherever it is
+    needed (see include/lora_linear.h): element e of the tensor has the bit that
+    lora_dropout_keep_mask gives it.  The call uses ceil(numel / 16) counters from
+    `offset` on; the gradient is the same call on dY without the residual.
+
+    X, Y, residual: tensors of one shape, torch.bfloat16 or torch.float32; Y may be X
+    or the residual itself."""
+    if _BF16 is None:
+        _bind_torch()
+    if X.dtype is not _BF16 and X.dtype is not _F32:
+        raise TypeError(f"X: expected torch.bfloat16 or torch.float32, got {X.dtype}")
+    for t, name in ((X, "X"), (Y, "Y"), (residual, "residual")):
+        if t is not None and not _fits(t, X.dtype, X.shape):
+            _check(t, name, X.dtype, X.shape)
+    st = load_library().lora_dropout(_ptr(X), _ptr(residual), _ptr(Y), 1 if X.dtype is _F32 else 0, X.numel(),
+                                     int(seed) & 0xFFFFFFFFFFFFFFFF, int(offset) & 0xFFFFFFFFFFFFFFFF, float(p),
+                                     _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_dropout")
+
+
+def lora_linear_xent_workspace_size(rows: int, vocab: int, k: int, dx: bool = False, dw: bool = False) -> int:
+    return int(load_library().lora_linear_xent_workspace_size(rows, vocab, k, int(dx), int(dw)))
+
+
+def _check_xent(X, W, labels):
+    if _BF16 is None:
+        _bind_torch()
+    rows, k = X.shape
+    vocab = W.shape[0]
+    _check_rows((X, "X", _BF16, (rows, k)), (W, "W", _BF16, (vocab, k)), (labels, "labels", _I32, (rows,)))
+    return rows, vocab, k
+
+
+def _check_xent_grads(dX, dW, dloss, rows, vocab, k):
+    _check_rows((dloss, "dloss", _F32, (rows,)))
+    if dX is not None:
+        _check_rows((dX, "dX", _BF16, (rows, k)))
+    if dW is not None:
+        _check_rows((dW, "dW", _BF16, (vocab, k)))
+
+
+def lora_linear_xent_fwd(X, W, labels, loss, saved, workspace, stream=None) -> None:
+    """Cross entropy of softmax(X W^T) against each row's label, without its logits
+    (see include/lora_linear.h), and what lora_linear_xent_bwd needs in `saved`.
+
+    X [rows,k], W [vocab,k]: torch.bfloat16; labels [rows]: torch.int32, one outside
+    the vocabulary (-100, for instance) is none; loss [rows], saved [rows,2] (or None):
+    torch.float32; workspace: a device tensor of at least
+    lora_linear_xent_workspace_size(rows, vocab, k) bytes."""
+    rows, vocab, k = _check_xent(X, W, labels)
+    _check_rows((loss, "loss", _F32, (rows,)))
+    if saved is not None:
+        _check_rows((saved, "saved", _F32, (rows, 2)))
+    ws_bytes = _workspace_bytes(workspace)
+    st = load_library().lora_linear_xent_fwd(_ptr(X), _ptr(W), _ptr(labels), _ptr(loss), _ptr(saved), _ptr(workspace),
+                                             ws_bytes, rows, vocab, k, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_linear_xent_fwd")
+
+
+def lora_linear_xent_bwd(X, W, labels, saved, dloss, dX, dW, workspace, stream=None) -> None:
+    """Gradients of lora_linear_xent_fwd's loss for an upstream dloss [rows]
+    (torch.float32): dX [rows,k] and dW [vocab,k], torch.bfloat16, one of them or both
+    (None: not formed).  workspace: lora_linear_xent_workspace_size(rows, vocab, k,
+    dX is not None, dW is not None) bytes."""
+    rows, vocab, k = _check_xent(X, W, labels)
+    _check_rows((saved, "saved", _F32, (rows, 2)))
+    _check_xent_grads(dX, dW, dloss, rows, vocab, k)
+    ws_bytes = _workspace_bytes(workspace)
+    st = load_library().lora_linear_xent_bwd(_ptr(X), _ptr(W), _ptr(labels), _ptr(saved), _ptr(dloss), _ptr(dX),
+                                             _ptr(dW), _ptr(workspace), ws_bytes, rows, vocab, k, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_linear_xent_bwd")
+
+
+def lora_linear_xent_step(X, W, labels, dloss, loss, dX, dW, workspace, stream=None) -> None:
+    """lora_linear_xent_fwd and lora_linear_xent_bwd in one call; without dW the logits
+    are formed once."""
+    rows, vocab, k = _check_xent(X, W, labels)
+    _check_rows((loss, "loss", _F32, (rows,)))
+    _check_xent_grads(dX, dW, dloss, rows, vocab, k)
+    ws_bytes = _workspace_bytes(workspace)
+    st = load_library().lora_linear_xent_step(_ptr(X), _ptr(W), _ptr(labels), _ptr(dloss), _ptr(loss), _ptr(dX), _ptr(dW),
+                                              _ptr(workspace), ws_bytes, rows, vocab, k, _stream_handle(stream))
+    if st != 0:
+        raise LoraError(st, "lora_linear_xent_step")
 
 
 def lora_linear_plan(op: str, m: int, n, k: int, r: int) -> list:

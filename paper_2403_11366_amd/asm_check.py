@@ -135,7 +135,7 @@ def check_first_reads(name: str, lines: list) -> list:
 
 
 # The 256 x 256 tiles (two LDS stages, wave rows taking turns).
-_TWO_STAGE = re.compile(r"lora_(?:fwd|bwd_dx)_kernel<256, 256,")
+_TWO_STAGE = re.compile(r"lora_(?:fwd|bwd_dx)_kernel<256, 256,|(?:logits|grad|fwd|bwd)_kernel<lora::N[tn]Big<")
 
 
 def is_two_stage(name: str) -> bool:

@@ -18,7 +18,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblora_linear.so")
 SOURCES = ["lora_abi.cpp", "lora_fwd.hip", "lora_fwd_skinny.hip", "lora_bwd.hip", "lora_merge.hip", "lora_mask.hip",
-           "lora_ops_abi.cpp", "lora_logits.hip", "lora_mx4.hip"]
+           "lora_ops_abi.cpp", "lora_logits.hip", "lora_mx4.hip", "lora_train_abi.cpp", "lora_fp8.hip", "lora_xent.hip",
+           "lora_dropout.hip"]
 
 
 def hipcc() -> str:

@@ -1,0 +1,277 @@
+// Matrices in 8-bit floating point (e4m3) with a scale 2^(s - 127) for each block of
+// 128: quantisation, its inverse, and the products of a frozen weight W [n, k],
+//   Y = Q(X) Q(W)^T,   dX = Q(dY) Q(W),
+// on the matrix cores' scaled 8-bit products (lora_gemm.hpp).  A weight's blocks are
+// 128 x 128, so that its scale is one number for a product of either direction;
+// activations have one per row.
+#include "lora_device.hpp"
+#include "lora_gemm.hpp"
+#include "lora_train.hpp"
+
+namespace lora {
+
+// The scale byte of a block from its largest magnitude's bf16 bits: the smallest s
+// with magnitude <= 448 2^(s - 127) (448 = 1.75 2^8: 1.75 has bits 0x60 after the
+// exponent), at least 0; 255 where the block holds a NaN or an infinity.
+__device__ __forceinline__ int fp8_scale(uint32_t top) {
+  const int field = (int)(top >> 7);
+  return field == 255 ? 255 : max(field - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0), 0);
+}
+__device__ __forceinline__ uint32_t top_of(const int4v& x) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const uint32_t w = (uint32_t)x[h] & 0x7FFF7FFFu;
+    top = max(top, max(w & 0xFFFFu, w >> 16));
+  }
+  return top;
+}
+// The largest of a value over 16 neighbouring lanes.
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true));    // lane ^ 1
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true));    // lane ^ 2
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true));   // 7 - lane of 8
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true));   // 15 - lane of 16
+}
+// Eight bf16 values' codes under a scale.  The division by the scale is exact (below
+// 2^-126 it is scaled up), the conversion rounds to nearest even and finds no value
+// beyond 448.
+__device__ __forceinline__ int2w fp8_codes(const int4v& x, int scale) {
+  const float up = __builtin_bit_cast(float, (uint32_t)(scale == 255 ? 0 : 254 - scale) << 23);
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = bf16_to_f32((u16)((uint32_t)x[e >> 1] >> (16 * (e & 1)))) * up;
+  int2w o{0, 0};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h], y[4 * h + 1], 0, false);
+    o[h] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2], y[4 * h + 3], w, true);
+  }
+  return scale == 255 ? int2w{0, 0} : o;
+}
+__device__ __forceinline__ int fp8_row_scale_at(int row, int block, int cells) {
+  return (block * cells + (row >> 6)) * 64 + (row & 15) * 4 + ((row >> 4) & 3);
+}
+
+// Activations: 16 lanes a row's block, 8 columns each.
+__global__ __launch_bounds__(256) void lora_fp8_quantize_rows_kernel(const u16* __restrict__ X,
+                                                                     uint8_t* __restrict__ codes,
+                                                                     uint8_t* __restrict__ scales, int rows, int k,
+                                                                     int blocks, int cells) {
+  const int64_t e = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int row = (int)(e / blocks), b = (int)(e - (int64_t)row * blocks);
+  if (row >= cells * 64) return;
+  const int j = threadIdx.x & 15, col = b * 128 + 8 * j;
+  int4v x{0, 0, 0, 0};
+  if (row < rows && col < k) x = *reinterpret_cast<const int4v*>(X + (size_t)row * k + col);
+  const int s = fp8_scale(max16(top_of(x)));
+  if (row < rows) *reinterpret_cast<int2w*>(codes + ((size_t)row * blocks + b) * 128 + 8 * j) = fp8_codes(x, s);
+  if (j == 0) scales[fp8_row_scale_at(row, b, cells)] = (uint8_t)(row < rows ? s : 0);
+}
+
+// A weight: a workgroup a block of 128 x 128.
+__global__ __launch_bounds__(256) void lora_fp8_quantize_block_kernel(const u16* __restrict__ X,
+                                                                      uint8_t* __restrict__ codes,
+                                                                      uint8_t* __restrict__ scales, int rows, int k,
+                                                                      int blocks) {
+  __shared__ uint32_t tops[4];
+  const int b = (int)blockIdx.x % blocks, r0 = (int)blockIdx.x / blocks * 128;
+  const int tid = threadIdx.x, j = tid & 15, col = b * 128 + 8 * j;
+  int4v x[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = r0 + (tid >> 4) + 16 * i;
+    x[i] = row < rows && col < k ? *reinterpret_cast<const int4v*>(X + (size_t)row * k + col) : int4v{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, top_of(x[i]));
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+  if ((tid & 63) == 0) tops[tid >> 6] = top;
+  __syncthreads();
+  const int s = fp8_scale(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+  if (tid == 0) scales[blockIdx.x] = (uint8_t)s;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = r0 + (tid >> 4) + 16 * i;
+    if (row < rows) *reinterpret_cast<int2w*>(codes + ((size_t)row * blocks + b) * 128 + 8 * j) = fp8_codes(x[i], s);
+  }
+}
+
+// The values of codes and scales: a lane takes 8 columns.
+template <bool ROWS>
+__global__ __launch_bounds__(256) void lora_fp8_dequantize_kernel(const uint8_t* __restrict__ codes,
+                                                                  const uint8_t* __restrict__ scales,
+                                                                  u16* __restrict__ X, int rows, int k, int blocks,
+                                                                  int cells) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int per = k / 8, row = (int)(e / per), piece = (int)(e - (int64_t)row * per);
+  if (row >= rows) return;
+  const int b = piece >> 4;
+  const int2w w = *reinterpret_cast<const int2w*>(codes + (size_t)row * blocks * 128 + 8 * piece);
+  const int s = scales[ROWS ? fp8_row_scale_at(row, b, cells) : (row >> 7) * blocks + b];
+  // 2^(s - 127); s = 0 is a subnormal, 255 NaN
+  const uint32_t bits = s == 0 ? 0x00400000u : (s == 255 ? 0x7FC00000u : (uint32_t)s << 23);
+  const float unit = __builtin_bit_cast(float, bits);
+  int4v o;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const auto v = h & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(w[h >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(w[h >> 1], false);
+    o[h] = (int)((uint32_t)f32_to_bf16(v[0] * unit) | ((uint32_t)f32_to_bf16(v[1] * unit) << 16));
+  }
+  *reinterpret_cast<int4v*>(X + (size_t)row * k + 8 * piece) = o;
+}
+
+// Stores a wave's sums as bf16 rows, straight from the registers.
+template <class Core>
+__device__ __forceinline__ void store_tile(const typename Core::Acc& acc, u16* out, int m, int n, int m0, int n0) {
+  constexpr int FA = sizeof(acc) / sizeof(acc[0]), FB = sizeof(acc[0]) / sizeof(acc[0][0]);
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
+#pragma unroll
+  for (int b = 0; b < FB; ++b) {
+    const int row = m0 + Core::row0(wave) + 16 * b + c16;
+#pragma unroll
+    for (int a = 0; a < FA; ++a) {
+      const int col = n0 + Core::col(wave, a) + 4 * g;
+      const floatx4 v = acc[a][b];
+      if (row < m && col < n)
+        *reinterpret_cast<uint2*>(out + (size_t)row * n + col) =
+            uint2{(uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
+                  (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16)};
+    }
+  }
+}
+
+struct Fp8Product {
+  const uint8_t *Ac, *As, *Wc, *Ws;
+  u16* out;
+  float* sums;
+  int m, n, k, tiles_m, tiles_n, splits;
+};
+
+template <class Core, int BM, int BN, int NT>
+__global__ __launch_bounds__(NT) void lora_fp8_fwd_kernel(Fp8Product p) {
+  __shared__ __attribute__((aligned(1024))) char smem[Core::SMEM];
+  int tm, tn;
+  tile_coords(p.tiles_m, p.tiles_n, 8, (int)blockIdx.x, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN, blocks = (p.k + 127) / 128;
+  const uint32_t row = (uint32_t)blocks * 128;
+  const NtTile t{make_rsrc(p.Ac + (size_t)m0 * row, (uint64_t)min(BM, p.m - m0) * row),
+                 make_rsrc(p.Wc + (size_t)n0 * row, (uint64_t)min(BN, p.n - n0) * row), row, row, row, blocks};
+  const int nb = (p.n + 127) / 128;
+  const Scales sc{p.As, p.Ws, (p.m + 63) / 64, nb * blocks, n0 / 128 * blocks, 1, blocks, nb - n0 / 128};
+  typename Core::Acc acc;
+  Core::run(t, sc, m0, smem, acc);
+  store_tile<Core>(acc, p.out, p.m, p.n, m0, n0);
+}
+
+template <class Core, int BM, int NT>
+__global__ __launch_bounds__(NT) void lora_fp8_bwd_kernel(Fp8Product p) {
+  __shared__ __attribute__((aligned(1024))) char smem[Core::SMEM];
+  int tm, tn;
+  const int tiles = p.tiles_m * p.tiles_n, split = (int)blockIdx.x / tiles;
+  tile_coords(p.tiles_m, p.tiles_n, 8, (int)blockIdx.x - split * tiles, tm, tn);
+  const int m0 = tm * BM, l0 = tn * 256, stages = (p.n + 127) / 128, kb = (p.k + 127) / 128;
+  const uint32_t arow = (uint32_t)stages * 128, brow = (uint32_t)kb * 128;
+  const NnTile t{make_rsrc(p.Ac + (size_t)m0 * arow, (uint64_t)min(BM, p.m - m0) * arow), arow,
+                 reinterpret_cast<const char*>(p.Wc) + l0, brow, (uint64_t)p.n * brow - l0, stages};
+  const Scales sc{p.As, p.Ws, (p.m + 63) / 64, stages * kb, l0 / 128, kb, 1, kb - l0 / 128};
+  typename Core::Acc acc;
+  const int s0 = (int)((int64_t)stages * split / p.splits), s1 = (int)((int64_t)stages * (split + 1) / p.splits);
+  Core::run(t, sc, m0, s0, s1, smem, acc);
+  if (p.splits == 1) {
+    store_tile<Core>(acc, p.out, p.m, p.k, m0, l0);
+  } else {   // [split][tile][row][column]
+    float* to = p.sums + ((size_t)split * tiles + (size_t)tm * p.tiles_n + tn) * BM * 256;
+    constexpr int FA = sizeof(acc) / sizeof(acc[0]), FB = sizeof(acc[0]) / sizeof(acc[0][0]);
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+#pragma unroll
+    for (int b = 0; b < FB; ++b)
+#pragma unroll
+      for (int a = 0; a < FA; ++a)
+        *reinterpret_cast<floatx4*>(to + (Core::row0(wave) + 16 * b + (lane & 15)) * 256 + Core::col(wave, a) +
+                                    4 * (lane >> 4)) = acc[a][b];
+  }
+}
+
+// The sum of a split product's parts, in their order: 4 columns a thread.
+__global__ __launch_bounds__(256) void lora_fp8_join_kernel(const float* __restrict__ sums, u16* __restrict__ out, int m,
+                                                            int k, int tiles_n, int tiles, int splits) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int per = k / 4, row = (int)(e / per), col = 4 * (int)(e - (int64_t)row * per);
+  if (row >= m) return;
+  const float* from = sums + ((size_t)(row / 64) * tiles_n + col / 256) * 64 * 256 + (row & 63) * 256 + (col & 255);
+  floatx4 v{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const floatx4*>(from + (size_t)s * tiles * 64 * 256);
+  *reinterpret_cast<uint2*>(out + (size_t)row * k + col) =
+      uint2{(uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
+            (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16)};
+}
+
+hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, hipStream_t st) {
+  const int blocks = (int)fp8_blocks(a.k), cells = (int)fp8_cells(a.rows);
+  if (a.block_rows == 1)
+    hipLaunchKernelGGL(lora_fp8_quantize_rows_kernel, dim3((unsigned)cdiv((int64_t)cells * 64 * blocks, 16)), dim3(256),
+                       0, st, a.X, a.codes, a.scales, (int)a.rows, (int)a.k, blocks, cells);
+  else
+    hipLaunchKernelGGL(lora_fp8_quantize_block_kernel, dim3((unsigned)(cdiv(a.rows, 128) * blocks)), dim3(256), 0, st,
+                       a.X, a.codes, a.scales, (int)a.rows, (int)a.k, blocks);
+  return hipGetLastError();
+}
+
+hipError_t launch_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, uint16_t* X, int64_t rows, int64_t k,
+                                 int block_rows, hipStream_t st) {
+  const dim3 grid((unsigned)cdiv(rows * (k / 8), 256));
+  if (block_rows == 1)
+    hipLaunchKernelGGL((lora_fp8_dequantize_kernel<true>), grid, dim3(256), 0, st, codes, scales, X, (int)rows, (int)k,
+                       (int)fp8_blocks(k), (int)fp8_cells(rows));
+  else
+    hipLaunchKernelGGL((lora_fp8_dequantize_kernel<false>), grid, dim3(256), 0, st, codes, scales, X, (int)rows, (int)k,
+                       (int)fp8_blocks(k), (int)fp8_cells(rows));
+  return hipGetLastError();
+}
+
+static hipError_t quantise_input(const Fp8Args& a, int64_t cols, const Fp8Layout& L, hipStream_t st) {
+  return launch_fp8_quantize(Fp8QuantArgs{a.A, reinterpret_cast<uint8_t*>(a.ws + L.codes),
+                                          reinterpret_cast<uint8_t*>(a.ws + L.scales), a.m, cols, 1}, st);
+}
+static Fp8Product product_of(const Fp8Args& a, const Fp8Layout& L, const Fp8Plan& p) {
+  return Fp8Product{reinterpret_cast<uint8_t*>(a.ws + L.codes), reinterpret_cast<uint8_t*>(a.ws + L.scales), a.Wc, a.Ws,
+                    a.out, reinterpret_cast<float*>(a.ws + L.sums), (int)a.m, (int)a.n, (int)a.k, p.tiles_m, p.tiles_n,
+                    p.splits};
+}
+
+hipError_t launch_fp8_fwd(const Fp8Args& a, hipStream_t st) {
+  const Fp8Layout L = fp8_fwd_layout(a.m, a.n, a.k);
+  const hipError_t e = quantise_input(a, a.k, L, st);
+  if (e != hipSuccess) return e;
+  const Fp8Plan p = plan_fp8_fwd(a.m, a.n, a.k);
+  const Fp8Product q = product_of(a, L, p);
+  if (p.kind == FP8_BIG)
+    hipLaunchKernelGGL((lora_fp8_fwd_kernel<NtBig<Fp8, false>, 256, 256, 512>), dim3((unsigned)p.grid), dim3(512), 0, st, q);
+  else
+    hipLaunchKernelGGL((lora_fp8_fwd_kernel<NtCore<Fp8, 64, 128, 1, 4, 3, false>, 64, 128, 256>), dim3((unsigned)p.grid),
+                       dim3(256), 0, st, q);
+  return hipGetLastError();
+}
+
+hipError_t launch_fp8_bwd(const Fp8Args& a, hipStream_t st) {
+  const Fp8Layout L = fp8_bwd_layout(a.m, a.n, a.k);
+  hipError_t e = quantise_input(a, a.n, L, st);
+  if (e != hipSuccess) return e;
+  const Fp8Plan p = plan_fp8_bwd(a.m, a.n, a.k);
+  const Fp8Product q = product_of(a, L, p);
+  if (p.kind == FP8_BIG)
+    hipLaunchKernelGGL((lora_fp8_bwd_kernel<NnBig<Fp8>, 256, 512>), dim3((unsigned)p.grid), dim3(512), 0, st, q);
+  else
+    hipLaunchKernelGGL((lora_fp8_bwd_kernel<NnCore<Fp8, 64, 256, 4, 3>, 64, 256>), dim3((unsigned)p.grid), dim3(256), 0,
+                       st, q);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  hipLaunchKernelGGL(lora_fp8_join_kernel, dim3((unsigned)cdiv(a.m * (a.k / 4), 256)), dim3(256), 0, st, q.sums, a.out,
+                     (int)a.m, (int)a.k, p.tiles_n, p.tiles_m * p.tiles_n, p.splits);
+  return hipGetLastError();
+}
+
+}  // namespace lora

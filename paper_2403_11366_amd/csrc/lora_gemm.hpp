@@ -1,0 +1,695 @@
+// Matrix product cores shared by the 8-bit linear layer (lora_fp8.hip) and the
+// cross entropy without logits (lora_xent.hip): output tiles of BM rows x BN
+// columns whose sums stay in registers, for an epilogue of the caller's.
+//
+//   nt_*:  C = A B^T, both operands' rows contiguous along the contraction
+//   nn_*:  C = A B,   A as above, B's rows contiguous along the columns
+//
+// A stage is 128 bytes of contraction of every k-contiguous row: 64 bf16 or 128
+// 8-bit elements.  Lane l (g = l / 16, c = l % 16) multiplies chunks g and g + 4 of
+// 16 bytes of a row's eight: two 16x16x32 bf16 products, or one 16x16x128 product
+// of 8 bits.  The order in which a product's contraction stands in the registers
+// is free as long as both operands agree on it, so both types share addresses,
+// copies and reads; the 8-bit ones' scales cover a whole stage (blocks of 128), so
+// they do not depend on it either.  (The 8-bit instruction adds the 16 products of a
+// chunk after cutting each, towards zero, to a multiple of 2^-13 of the largest one's
+// power of two -- a product has 8 significant bits, so only those below 2^-7 of the
+// largest lose any -- and chunks in fp32: measured by products that cancel.  On normal
+// values that is far below the result's rounding to bf16.)  Products are formed transposed (B as the A
+// operand), so a lane's sums are 4 consecutive columns of one row:
+//   acc[a][b] of lane l: row 16 b + c of the wave's, columns 4 g .. 4 g + 3 of
+//   fragment a.
+#pragma once
+
+#include <type_traits>
+#include <utility>
+
+#include "lora_device.hpp"
+
+namespace lora {
+
+typedef int int8v __attribute__((ext_vector_type(8)));
+typedef int int2w __attribute__((ext_vector_type(2)));
+
+template <typename F, int... I>
+__device__ __forceinline__ void each_index(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+// f(0), ..., f(N - 1) with compile-time arguments.
+template <int N, typename F>
+__device__ __forceinline__ void each_of(F&& f) {
+  each_index(std::make_integer_sequence<int, N>{}, f);
+}
+
+struct Bf16 {
+  static constexpr int BYTES = 2, KS = 64;   // of an element; elements of a stage
+  static constexpr bool SCALED = false;
+};
+struct Fp8 {   // e4m3
+  static constexpr int BYTES = 1, KS = 128;
+  static constexpr bool SCALED = true;
+};
+
+struct Frag {   // of 16 rows (or columns) x a stage
+  int4v lo, hi;
+};
+
+// The sums are formed here, and not where a caller's branch on a lane's row or column
+// first uses them: a product reads registers (the scales among them) of lanes that
+// such a branch has switched off.
+template <int FA, int FB>
+__device__ __forceinline__ void formed(floatx4 (&acc)[FA][FB]) {
+#pragma unroll
+  for (int a = 0; a < FA; ++a)
+#pragma unroll
+    for (int b = 0; b < FB; ++b) asm volatile("" : "+v"(acc[a][b]));
+}
+
+// acc += A B^T of a stage; SB picks the byte of sb (the rows' scales), sa is the
+// columns'.
+template <class E, int SB>
+__device__ __forceinline__ floatx4 stage_product(const Frag& a, const Frag& b, floatx4 acc, int sa, int sb) {
+  if constexpr (E::SCALED) {
+    const int8v A{a.lo[0], a.lo[1], a.lo[2], a.lo[3], a.hi[0], a.hi[1], a.hi[2], a.hi[3]};
+    const int8v B{b.lo[0], b.lo[1], b.lo[2], b.lo[3], b.hi[0], b.hi[1], b.hi[2], b.hi[3]};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc, 0, 0, 0, sa, SB, sb);
+  } else {
+    acc = mfma16x16x32(__builtin_bit_cast(short8, a.lo), __builtin_bit_cast(short8, b.lo), acc);
+    return mfma16x16x32(__builtin_bit_cast(short8, a.hi), __builtin_bit_cast(short8, b.hi), acc);
+  }
+}
+
+// Scales of 8-bit operands.  A's (activations): a word per 16-row position of a
+// 64-row cell, cells [stage][cells]; B's (a weight): one byte per 128 x 128 block.
+struct Scales {
+  const uint8_t* a;
+  const uint8_t* b;
+  int cells;      // 64-row cells of A
+  int b_blocks;   // scale bytes of B
+  int b_first;    // B: byte of (this tile's first column block, stage 0)
+  int b_step;     // from stage to stage
+  int b_col;      // from column block to column block
+  int b_cols;     // column blocks from this tile's first on (clamped to)
+};
+
+// A lane's offset in a stage's scales of A: words of `count` cells from `first` on,
+// past them and past the operand kOOB.
+__device__ __forceinline__ uint32_t scale_words(const Scales& s, int first, int count, int lane) {
+  return lane < 16 * count && first + (lane >> 4) < s.cells ? (uint32_t)first * 64 + 4 * lane : kOOB;
+}
+
+// A tile's operands.
+struct NtTile {
+  __amdgpu_buffer_rsrc_t a, b;    // from the tile's first row, and column, on
+  uint32_t a_row, b_row;          // bytes of a row
+  uint32_t kbytes;                // of them to contract
+  int stages;
+};
+struct NnTile {
+  __amdgpu_buffer_rsrc_t a;       // from the tile's first row on
+  uint32_t a_row;
+  const char* b;                  // column of the tile's first, row 0 of the contraction
+  uint32_t b_row;
+  uint64_t b_bytes;               // from b to the operand's end
+  int stages;
+};
+// B's rows of stage kb: what is left of the operand, at most a stage of rows.
+template <class E>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t nn_rows(const NnTile& t, int kb) {
+  const uint64_t at = (uint64_t)kb * E::KS * t.b_row;
+  const uint64_t left = t.b_bytes > at ? t.b_bytes - at : 0, most = (uint64_t)E::KS * t.b_row;
+  return make_rsrc(t.b + (left ? at : 0), left < most ? left : most);
+}
+
+// The weight's scale bytes of up to 64 stages in one register, a stage to a lane
+// (with two column blocks a stage: 32 stages, two lanes each).
+template <int COLS>
+struct BScales {
+  int lanes = 0, base = 0;
+  static constexpr int SPAN = 64 / COLS;
+  __device__ __forceinline__ void load(const Scales& s, int col, int kb, int stages, int lane) {
+    base = kb;
+    const int st = min(kb + lane / COLS, stages - 1), cb = min(col + lane % COLS, s.b_cols - 1);
+    lanes = s.b[(size_t)s.b_first + (size_t)st * s.b_step + (size_t)cb * s.b_col];
+    asm volatile("" : "+v"(lanes));   // waited for here, once, and not at every use
+  }
+  __device__ __forceinline__ int at(int kb, int col) const {
+    return __builtin_amdgcn_readlane(lanes, (kb - base) * COLS + col);
+  }
+};
+
+// ---------------------------------------------------------------------------
+// C = A B^T, BM x BN by WM x WN waves, NS stages of LDS copied from memory straight
+// into LDS, one barrier a stage.
+template <class E, int BM, int BN, int WM, int WN, int NS, bool TAIL>
+struct NtCore {
+  static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FA = TN / 16, FB = TM / 16;
+  static constexpr int CX = BM / 8 / NW, CB = BN / 8 / NW, CS = E::SCALED ? 1 : 0, C = CX + CB + CS;
+  static constexpr int SOFF = (BM + BN) * 128, STAGE = SOFF + CS * NW * 256, SMEM = NS * STAGE;
+  static_assert(TM % 64 == 0 && TN % 16 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (NS - 1) * C < 64, "tile");
+  typedef floatx4 Acc[FA][FB];
+  static __device__ __forceinline__ int row0(int wave) { return wave / WN * TM; }
+  static __device__ __forceinline__ int col(int wave, int a) { return wave % WN * TN + 16 * a; }
+
+  static __device__ __forceinline__ void run(const NtTile& t, const Scales& sc, int m0, char* smem, Acc& acc) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN, g = lane >> 4, c16 = lane & 15, l8 = lane >> 3;
+#pragma unroll
+    for (int a = 0; a < FA; ++a)
+#pragma unroll
+      for (int b = 0; b < FB; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const int crow = 8 * wave;
+    const uint32_t kcol = (uint32_t)(((lane & 7) ^ kc_swz(crow + l8)) << 4);
+    const uint32_t aoff = (uint32_t)(crow + l8) * t.a_row + kcol, boff = (uint32_t)(crow + l8) * t.b_row + kcol;
+    __amdgpu_buffer_rsrc_t rsS = t.a;
+    uint32_t soff = kOOB;
+    BScales<1> bs;
+    const int bcol = wn * TN / 128;
+    if constexpr (E::SCALED) {
+      rsS = make_rsrc(sc.a, (uint64_t)sc.cells * t.stages * 64);
+      soff = scale_words(sc, m0 / 64 + wm * (TM / 64), TM / 64, lane);
+    }
+    auto copy = [&](int kb) LORA_INLINE {   // past the last stage: zeros, so that the counts hold
+      char* sb = smem + kb % NS * STAGE;
+      const bool live = kb < t.stages;
+      const uint32_t at = live ? (uint32_t)kb * 128 : 0u;
+      const bool in = live && (!TAIL || at + kcol < t.kbytes);
+#pragma unroll
+      for (int i = 0; i < CX; ++i)
+        dma16(t.a, in ? aoff + (uint32_t)(8 * NW * i) * t.a_row : kOOB, at, sb + (crow + 8 * NW * i) * 128);
+#pragma unroll
+      for (int i = 0; i < CB; ++i)
+        dma16(t.b, in ? boff + (uint32_t)(8 * NW * i) * t.b_row : kOOB, at, sb + (BM + crow + 8 * NW * i) * 128);
+      if constexpr (E::SCALED)
+        dma4(rsS, live ? soff : kOOB, live ? (uint32_t)kb * sc.cells * 64 : 0u, sb + SOFF + wave * 256);
+    };
+    if constexpr (E::SCALED) bs.load(sc, bcol, 0, t.stages, lane);
+#pragma unroll
+    for (int j = 0; j < NS - 1; ++j) copy(j);
+    for (int kb = 0; kb < t.stages; ++kb) {
+      if constexpr (E::SCALED)
+        if (kb - bs.base == bs.SPAN) bs.load(sc, bcol, kb, t.stages, lane);
+      copy_barrier<(NS - 2) * C>();   // this stage has landed, and every wave has read the one before
+      copy(kb + NS - 1);
+      const char* sb = smem + kb % NS * STAGE;
+      int sa = 0, sw[TM / 64] = {};
+      if constexpr (E::SCALED) {
+        sa = bs.at(kb, 0);
+#pragma unroll
+        for (int i = 0; i < TM / 64; ++i)
+          sw[i] = *reinterpret_cast<const int*>(sb + SOFF + wave * 256 + i * 64 + c16 * 4);
+      }
+      Frag fa[FA];
+#pragma unroll
+      for (int a = 0; a < FA; ++a) {
+        fa[a].lo = __builtin_bit_cast(int4v, kc_read(sb + BM * 128, wn * TN + 16 * a + c16, g));
+        fa[a].hi = __builtin_bit_cast(int4v, kc_read(sb + BM * 128, wn * TN + 16 * a + c16, 4 + g));
+      }
+      each_of<FB>([&](auto bc) LORA_INLINE {
+        constexpr int B = decltype(bc)::value;
+        Frag fb;
+        fb.lo = __builtin_bit_cast(int4v, kc_read(sb, wm * TM + 16 * B + c16, g));
+        fb.hi = __builtin_bit_cast(int4v, kc_read(sb, wm * TM + 16 * B + c16, 4 + g));
+#pragma unroll
+        for (int a = 0; a < FA; ++a) acc[a][B] = stage_product<E, B & 3>(fa[a], fb, acc[a][B], sa, sw[B >> 2]);
+      });
+    }
+    formed(acc);
+    copy_barrier<0>();   // the trailing copies have landed before the LDS is used again
+  }
+};
+
+// ---------------------------------------------------------------------------
+// LDS reads that transpose, for operands whose rows run along the columns.  16
+// bits: 16 lanes take 4 rows x 16 columns, 8 bits: 8 rows x 16 columns, and lane i
+// receives column i.
+template <class E, int OFF>
+__device__ __forceinline__ void read_tr_asm(int2w& d, uint32_t addr) {
+  if constexpr (E::BYTES == 1)
+    asm volatile("ds_read_b64_tr_b8 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "i"(OFF));
+  else
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "i"(OFF));
+}
+
+// Swizzle of the 8-bit rows of 128 bytes: the 16 rows that a half wave reads (8 of
+// one g, 8 of the next) fall into different banks.
+__device__ __forceinline__ int mc8_swz(int row) { return ((row >> 1) & 3) + 4 * ((row >> 4) & 1); }
+
+// The places of a stage of B, in panels of 128 columns: rows of 256 bytes (bf16,
+// 64 rows) or 128 bytes (8 bits, 128 rows), 16 KiB a panel.
+template <class E>
+struct Panel {
+  static constexpr int ROW = 128 * E::BYTES, CHUNKS = ROW / 16, RPC = 64 / CHUNKS;   // rows per copy of 1 KiB
+  static __device__ __forceinline__ int swz(int row) { return E::BYTES == 1 ? mc8_swz(row) : mc16_swz(row); }
+  // Address of the first read of the fragment at column chunk `chunk` (of 16 columns);
+  // the others are 1024, 8192 and 9216 bytes further (registers in that order).
+  static __device__ __forceinline__ uint32_t read_at(int frag, int lane) {
+    const int g = lane >> 4, j = lane & 15;
+    if constexpr (E::BYTES == 1) {
+      const int row = 16 * g + (j >> 1);
+      return (uint32_t)(row * ROW + ((frag ^ swz(row)) << 4) + (j & 1) * 8);
+    } else {
+      const int row = 8 * g + (j >> 2), q = j & 3;
+      return (uint32_t)(row * ROW + (((2 * frag + (q >> 1)) ^ swz(row)) << 4) + (q & 1) * 8);
+    }
+  }
+};
+
+// C = A B, BM x BN (BN 128 or 256) by WN waves along the columns, NS stages.
+template <class E, int BM, int BN, int WN, int NS>
+struct NnCore {
+  static constexpr int NW = WN, TN = BN / WN, FA = TN / 16, FB = BM / 16;
+  static constexpr int CX = BM / 8 / NW, CB = BN * 128 / 1024 / NW, CS = E::SCALED ? 1 : 0, C = CX + CB + CS;
+  static constexpr int SOFF = (BM + BN) * 128, STAGE = SOFF + CS * NW * 256, SMEM = NS * STAGE;
+  static_assert(BM == 64 && BN % 128 == 0 && TN % 16 == 0 && 128 % TN == 0 && (NS - 1) * C < 64, "tile");
+  typedef floatx4 Acc[FA][FB];
+  static __device__ __forceinline__ int row0(int) { return 0; }
+  static __device__ __forceinline__ int col(int wave, int a) { return wave * TN + 16 * a; }
+
+  // stages [s0, s1) of the contraction
+  static __device__ __forceinline__ void run(const NnTile& t, const Scales& sc, int m0, int s0, int s1, char* smem,
+                                             Acc& acc) {
+    using P = Panel<E>;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int g = lane >> 4, c16 = lane & 15, l8 = lane >> 3;
+#pragma unroll
+    for (int a = 0; a < FA; ++a)
+#pragma unroll
+      for (int b = 0; b < FB; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const int crow = 8 * wave;
+    const uint32_t kcol = (uint32_t)(((lane & 7) ^ kc_swz(crow + l8)) << 4);
+    const uint32_t aoff = (uint32_t)(crow + l8) * t.a_row + kcol;
+    __amdgpu_buffer_rsrc_t rsS = t.a;
+    uint32_t soff = kOOB;
+    BScales<1> bs;
+    const int bcol = wave * TN / 128;
+    if constexpr (E::SCALED) {
+      rsS = make_rsrc(sc.a, (uint64_t)sc.cells * t.stages * 64);
+      soff = scale_words(sc, m0 / 64, BM / 64, lane);
+    }
+    auto copy = [&](int kb) LORA_INLINE {
+      char* sb = smem + (kb - s0) % NS * STAGE;
+      const bool live = kb < s1;
+      const uint32_t at = live ? (uint32_t)kb * 128 : 0u;
+#pragma unroll
+      for (int i = 0; i < CX; ++i)
+        dma16(t.a, live ? aoff + (uint32_t)(8 * NW * i) * t.a_row : kOOB, at, sb + (crow + 8 * NW * i) * 128);
+      const __amdgpu_buffer_rsrc_t rsB = nn_rows<E>(t, live ? kb : s0);
+#pragma unroll
+      for (int i = 0; i < CB; ++i) {
+        const int q = wave + NW * i, p = q >> 4, row = (q & 15) * P::RPC + lane / P::CHUNKS;   // 16 copies a panel
+        const int ch = lane % P::CHUNKS ^ P::swz(row);
+        dma16(rsB, live ? (uint32_t)row * t.b_row + (uint32_t)(p * P::ROW + 16 * ch) : kOOB, 0,
+              sb + BM * 128 + q * 1024);
+      }
+      if constexpr (E::SCALED)
+        dma4(rsS, live ? soff : kOOB, live ? (uint32_t)kb * sc.cells * 64 : 0u, sb + SOFF + wave * 256);
+    };
+    if constexpr (E::SCALED) bs.load(sc, bcol, s0, t.stages, lane);
+    uint32_t wa[FA];
+#pragma unroll
+    for (int a = 0; a < FA; ++a) {
+      const int f = (wave * TN + 16 * a) / 16;
+      wa[a] = lds_addr(smem + BM * 128 + (f >> 3) * 16384) + P::read_at(f & 7, lane);
+    }
+#pragma unroll
+    for (int j = 0; j < NS - 1; ++j) copy(s0 + j);
+    for (int kb = s0; kb < s1; ++kb) {
+      if constexpr (E::SCALED)
+        if (kb - bs.base == bs.SPAN) bs.load(sc, bcol, kb, t.stages, lane);
+      copy_barrier<(NS - 2) * C>();
+      copy(kb + NS - 1);
+      const int here = (kb - s0) % NS * STAGE;
+      const char* sb = smem + here;
+      int sa = 0, sw = 0;
+      if constexpr (E::SCALED) {
+        sa = bs.at(kb, 0);
+        sw = *reinterpret_cast<const int*>(sb + SOFF + wave * 256 + c16 * 4);
+      }
+      Frag fb[FB];
+#pragma unroll
+      for (int b = 0; b < FB; ++b) {
+        fb[b].lo = __builtin_bit_cast(int4v, kc_read(sb, 16 * b + c16, g));
+        fb[b].hi = __builtin_bit_cast(int4v, kc_read(sb, 16 * b + c16, 4 + g));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      int2w w[FA][4];
+#pragma unroll
+      for (int a = 0; a < FA; ++a) {
+        const uint32_t at = wa[a] + (uint32_t)here;
+        read_tr_asm<E, 0>(w[a][0], at);
+        read_tr_asm<E, 1024>(w[a][1], at);
+        read_tr_asm<E, 8192>(w[a][2], at);
+        read_tr_asm<E, 9216>(w[a][3], at);
+      }
+      if constexpr (FA == 4)
+        asm volatile("s_waitcnt lgkmcnt(0)"
+                     : "+v"(w[0][0]), "+v"(w[0][1]), "+v"(w[0][2]), "+v"(w[0][3]), "+v"(w[1][0]), "+v"(w[1][1]),
+                       "+v"(w[1][2]), "+v"(w[1][3]), "+v"(w[2][0]), "+v"(w[2][1]), "+v"(w[2][2]), "+v"(w[2][3]),
+                       "+v"(w[3][0]), "+v"(w[3][1]), "+v"(w[3][2]), "+v"(w[3][3]));
+      else
+        asm volatile("s_waitcnt lgkmcnt(0)"
+                     : "+v"(w[0][0]), "+v"(w[0][1]), "+v"(w[0][2]), "+v"(w[0][3]), "+v"(w[1][0]), "+v"(w[1][1]),
+                       "+v"(w[1][2]), "+v"(w[1][3]));
+      static_assert(FA == 4 || FA == 2, "the wait's operands");
+      __builtin_amdgcn_sched_barrier(0);
+      each_of<FB>([&](auto bc) LORA_INLINE {
+        constexpr int B = decltype(bc)::value;
+#pragma unroll
+        for (int a = 0; a < FA; ++a) {
+          Frag f;
+          f.lo = int4v{w[a][0].x, w[a][0].y, w[a][1].x, w[a][1].y};
+          f.hi = int4v{w[a][2].x, w[a][2].y, w[a][3].x, w[a][3].y};
+          acc[a][B] = stage_product<E, B & 3>(f, fb[B], acc[a][B], sa, sw);
+        }
+      });
+    }
+    formed(acc);
+    copy_barrier<0>();
+  }
+};
+
+// ---------------------------------------------------------------------------
+// The 256 x 256 tiles: eight waves in two rows of 128 x 64, two stages in LDS.  The
+// wave rows take turns: waves w and w + 4 share a SIMD, and while one multiplies,
+// the other reads its next fragments and issues copies; a workgroup barrier ends
+// each slot, and the second row runs one slot behind.  A stage is four phases, each
+// a slot of reads and a slot of products: (B half 0, A half 0), (B 1, A 0), (B 0, A
+// 1), (B 1, A 1), reading A half 0, B half 1, A half 1 and the next stage's B half
+// 0.  Every wave waits for its reads before the barrier that ends its read slot, so
+// the quarter of a stage read in phase P is free from the read slots of phase P + 1
+// on, which refill it for the stage after next.  The reads before the first slot
+// are closed the same way, by a barrier of all eight waves before the second row's
+// extra one.
+//
+// Copies of a wave in issue order: B half 0 (2), its rows' scales (S: 1 with 8 bits,
+// else 0) and A half 0 (2), B half 1 (2), A half 1 (2).  A phase's read slot waits
+// for the quarter read in the next phase; the newer ones may be under way.
+template <int N>
+using Count = std::integral_constant<int, N>;
+constexpr int kBigStage = 512 * 128;   // bytes of a stage
+
+// Runs the phases: F has read_a(kb, half), read_b(kb, Count<half>), copy_a, copy_b
+// (kb, half), wait_b(Count<half>) (-1: no fragments pass through the wait) and
+// products(hb, ha).
+template <int S, class F>
+__device__ __forceinline__ void big_phases(F& f, int stages, int wm) {
+  auto slot_end = [&]() LORA_INLINE {
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto ready = [&](auto left, auto half) LORA_INLINE {
+    __builtin_amdgcn_sched_barrier(0);
+    f.wait_b(half);
+    wait_vmcnt<decltype(left)::value>();
+    slot_end();
+  };
+  auto multiply = [&](auto hb, auto ha) LORA_INLINE {
+    f.products(hb, ha);
+    __builtin_amdgcn_sched_barrier(0);
+    slot_end();
+  };
+  using N1 = Count<-1>;
+  using I0 = Count<0>;
+  using I1 = Count<1>;
+  auto stage = [&](int kb, auto mode) LORA_INLINE {   // 0: steady, 1: the last but one, 2: the last
+    constexpr int MODE = decltype(mode)::value;
+    f.read_a(kb, 0);
+    if constexpr (MODE == 0) { f.copy_b(kb + 2, 0); ready(Count<12 + S>{}, N1{}); }
+    else if constexpr (MODE == 1) ready(Count<10 + S>{}, N1{});
+    else ready(Count<2>{}, N1{});
+    multiply(I0{}, I0{});
+    f.read_b(kb, I1{});
+    if constexpr (MODE == 0) { f.copy_a(kb + 2, 0); ready(Count<12 + 2 * S>{}, I1{}); }
+    else if constexpr (MODE == 1) ready(Count<8 + S>{}, I1{});
+    else ready(I0{}, I1{});
+    multiply(I1{}, I0{});
+    f.read_a(kb, 1);
+    if constexpr (MODE == 0) { f.copy_b(kb + 2, 1); ready(Count<12 + 2 * S>{}, N1{}); }
+    else if constexpr (MODE == 1) ready(Count<6 + S>{}, N1{});
+    else ready(I0{}, N1{});
+    multiply(I0{}, I1{});
+    if constexpr (MODE < 2) f.read_b(kb + 1, I0{});
+    if constexpr (MODE == 0) { f.copy_a(kb + 2, 1); ready(Count<12 + S>{}, I0{}); }
+    else if constexpr (MODE == 1) ready(Count<4>{}, I0{});
+    else ready(I0{}, N1{});
+    multiply(I1{}, I1{});
+  };
+  auto fill = [&](int kb) LORA_INLINE { f.copy_b(kb, 0); f.copy_a(kb, 0); f.copy_b(kb, 1); f.copy_a(kb, 1); };
+  fill(0);
+  if (stages > 1) {
+    fill(1);
+    wait_vmcnt<12 + S>();
+  } else {
+    wait_vmcnt<0>();
+  }
+  slot_end();
+  f.read_b(0, I0{});
+  __builtin_amdgcn_sched_barrier(0);
+  f.wait_b(I0{});
+  slot_end();                    // every wave has read the quarter that the first read slot refills
+  if (wm == 1) slot_end();       // the second wave row runs one slot behind
+  int kb = 0;
+  for (; kb + 2 < stages; ++kb) {
+    f.reload(kb);
+    stage(kb, I0{});
+  }
+  f.reload_end(kb);
+  if (stages > 1) stage(kb++, I1{});
+  stage(kb, Count<2>{});
+  if (wm == 0) slot_end();
+}
+
+template <class E>
+struct BigBase {
+  static constexpr int CS = E::SCALED ? 1 : 0;
+  static constexpr int SMEM = 2 * kBigStage + CS * 2 * 8 * 256;
+  typedef floatx4 Acc[4][8];
+  static __device__ __forceinline__ int row0(int wave) { return (wave >> 2) * 128; }
+};
+
+template <class E, bool TAIL>
+struct NtBig : BigBase<E> {
+  static __device__ __forceinline__ int col(int wave, int a) { return (wave & 3) * 64 + 16 * a; }
+
+  struct Loop {
+    const NtTile& t;
+    const Scales& sc;
+    floatx4 (&acc)[4][8];
+    char* smem;
+    __amdgpu_buffer_rsrc_t rsS;
+    int wm, wn, g, c16, lane, wave, bcol;
+    uint32_t aoff, boff, kcol, soff;
+    int arow, brow;                  // this wave's first tile row of a copy
+    Frag fb[2][2], fa[4];            // B halves, the current A half
+    int sw[2], sa;
+    BScales<1> bs;
+
+    __device__ __forceinline__ void reload(int kb) {
+      if constexpr (E::SCALED)
+        if (kb - bs.base == bs.SPAN) bs.load(sc, bcol, kb, t.stages, lane);
+    }
+    __device__ __forceinline__ void reload_end(int kb) {
+      if constexpr (E::SCALED) bs.load(sc, bcol, kb, t.stages, lane);
+    }
+    __device__ __forceinline__ void copy_a(int kb, int h) {
+      char* sb = smem + (kb & 1) * kBigStage + arow * 128 + h * 8192;
+      if constexpr (E::SCALED)
+        if (h == 0)
+          dma4(rsS, soff, (uint32_t)kb * sc.cells * 64, smem + 2 * kBigStage + ((kb & 1) * 8 + wave) * 256);
+      const bool ok = !TAIL || (uint32_t)kb * 128 + kcol < t.kbytes;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        dma16(t.a, ok ? aoff + (uint32_t)(64 * h + 128 * i) * t.a_row : kOOB, (uint32_t)kb * 128, sb + i * 16384);
+    }
+    __device__ __forceinline__ void copy_b(int kb, int h) {
+      char* sb = smem + (kb & 1) * kBigStage + 256 * 128 + brow * 128 + h * 4096;
+      const bool ok = !TAIL || (uint32_t)kb * 128 + kcol < t.kbytes;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        dma16(t.b, ok ? boff + (uint32_t)(32 * h + 128 * i) * t.b_row : kOOB, (uint32_t)kb * 128, sb + i * 16384);
+    }
+    __device__ __forceinline__ void read_a(int kb, int h) {
+      const char* As = smem + (kb & 1) * kBigStage;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        fa[b].lo = __builtin_bit_cast(int4v, kc_read(As, wm * 128 + 64 * h + 16 * b + c16, g));
+        fa[b].hi = __builtin_bit_cast(int4v, kc_read(As, wm * 128 + 64 * h + 16 * b + c16, 4 + g));
+      }
+      if constexpr (E::SCALED)
+        if (h == 0) {
+          const char* ss = smem + 2 * kBigStage + ((kb & 1) * 8 + wave) * 256 + c16 * 4;
+          sw[0] = *reinterpret_cast<const int*>(ss);
+          sw[1] = *reinterpret_cast<const int*>(ss + 64);
+          sa = bs.at(kb, 0);
+        }
+    }
+    template <int H>
+    __device__ __forceinline__ void read_b(int kb, Count<H>) {
+      const char* Bs = smem + (kb & 1) * kBigStage + 256 * 128;
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        fb[H][a].lo = __builtin_bit_cast(int4v, kc_read(Bs, wn * 64 + 32 * H + 16 * a + c16, g));
+        fb[H][a].hi = __builtin_bit_cast(int4v, kc_read(Bs, wn * 64 + 32 * H + 16 * a + c16, 4 + g));
+      }
+    }
+    template <int H>
+    __device__ __forceinline__ void wait_b(Count<H>) { wait_lgkm0(); }
+    template <int HB, int HA>
+    __device__ __forceinline__ void products(Count<HB>, Count<HA>) {
+      each_of<4>([&](auto bc) LORA_INLINE {
+        constexpr int B = decltype(bc)::value;
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+          acc[2 * HB + a][4 * HA + B] = stage_product<E, B>(fb[HB][a], fa[B], acc[2 * HB + a][4 * HA + B], sa, sw[HA]);
+      });
+    }
+  };
+
+  static __device__ __forceinline__ void run(const NtTile& t, const Scales& sc, int m0, char* smem,
+                                             floatx4 (&acc)[4][8]) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+      for (int b = 0; b < 8; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    Loop f{t, sc, acc, smem, t.a, wave >> 2, wave & 3, lane >> 4, lane & 15, lane, wave, (wave & 3) >> 1};
+    const int l8 = lane >> 3;
+    f.arow = 8 * wave;
+    f.brow = 64 * (wave >> 2) + 8 * (wave & 3);
+    f.kcol = (uint32_t)(((lane & 7) ^ kc_swz(f.arow + l8)) << 4);
+    f.aoff = (uint32_t)(f.arow + l8) * t.a_row + f.kcol;
+    f.boff = (uint32_t)(f.brow + l8) * t.b_row + f.kcol;
+    if constexpr (E::SCALED) {
+      f.rsS = make_rsrc(sc.a, (uint64_t)sc.cells * t.stages * 64);
+      f.soff = scale_words(sc, m0 / 64 + 2 * f.wm, 2, lane);
+      f.bs.load(sc, f.bcol, 0, t.stages, lane);
+    }
+    big_phases<BigBase<E>::CS>(f, t.stages, f.wm);
+    formed(acc);
+  }
+};
+
+// B's panels of 128 columns are its halves: wave column wn takes columns 32 wn ..
+// + 31 of both.
+template <class E>
+struct NnBig : BigBase<E> {
+  static __device__ __forceinline__ int col(int wave, int a) { return 128 * (a >> 1) + 32 * (wave & 3) + 16 * (a & 1); }
+
+  struct Loop {
+    using P = Panel<E>;
+    const NnTile& t;
+    const Scales& sc;
+    floatx4 (&acc)[4][8];
+    char* smem;
+    __amdgpu_buffer_rsrc_t rsS;
+    int wm, wn, g, c16, lane, wave, s0;   // s0: the first stage of the contraction
+    uint32_t aoff, boff, soff;
+    uint32_t wa[2];
+    Frag fa[4];
+    int2w w[2][2][4];                // B halves: [half][fragment][read]
+    int sw[2], sa[2];
+    BScales<2> bs;
+
+    __device__ __forceinline__ void reload(int kb) {
+      if constexpr (E::SCALED)
+        if (s0 + kb - bs.base == bs.SPAN) bs.load(sc, 0, s0 + kb, t.stages, lane);
+    }
+    __device__ __forceinline__ void reload_end(int kb) {
+      if constexpr (E::SCALED) bs.load(sc, 0, s0 + kb, t.stages, lane);
+    }
+    __device__ __forceinline__ void copy_a(int kb, int h) {
+      char* sb = smem + (kb & 1) * kBigStage + wave * 1024 + h * 8192;
+      if constexpr (E::SCALED)
+        if (h == 0)
+          dma4(rsS, soff, (uint32_t)(s0 + kb) * sc.cells * 64, smem + 2 * kBigStage + ((kb & 1) * 8 + wave) * 256);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        dma16(t.a, aoff + (uint32_t)(64 * h + 128 * i) * t.a_row, (uint32_t)(s0 + kb) * 128, sb + i * 16384);
+    }
+    __device__ __forceinline__ void copy_b(int kb, int h) {
+      char* sb = smem + (kb & 1) * kBigStage + 256 * 128 + h * 16384 + wave * 1024;
+      const __amdgpu_buffer_rsrc_t rs = nn_rows<E>(t, s0 + kb);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        dma16(rs, boff + (uint32_t)(8 * P::RPC * i) * t.b_row + (uint32_t)(h * P::ROW), 0, sb + i * 8192);
+    }
+    __device__ __forceinline__ void read_a(int kb, int h) {
+      const char* As = smem + (kb & 1) * kBigStage;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        fa[b].lo = __builtin_bit_cast(int4v, kc_read(As, wm * 128 + 64 * h + 16 * b + c16, g));
+        fa[b].hi = __builtin_bit_cast(int4v, kc_read(As, wm * 128 + 64 * h + 16 * b + c16, 4 + g));
+      }
+      if constexpr (E::SCALED)
+        if (h == 0) {
+          const char* ss = smem + 2 * kBigStage + ((kb & 1) * 8 + wave) * 256 + c16 * 4;
+          sw[0] = *reinterpret_cast<const int*>(ss);
+          sw[1] = *reinterpret_cast<const int*>(ss + 64);
+          sa[0] = bs.at(s0 + kb, 0);
+          sa[1] = bs.at(s0 + kb, 1);
+        }
+    }
+    template <int H>
+    __device__ __forceinline__ void read_b(int kb, Count<H>) {
+      const uint32_t o = (uint32_t)((kb & 1) * kBigStage);
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        read_tr_asm<E, H * 16384>(w[H][a][0], wa[a] + o);
+        read_tr_asm<E, H * 16384 + 1024>(w[H][a][1], wa[a] + o);
+        read_tr_asm<E, H * 16384 + 8192>(w[H][a][2], wa[a] + o);
+        read_tr_asm<E, H * 16384 + 9216>(w[H][a][3], wa[a] + o);
+      }
+    }
+    // The B fragments pass through the wait, so that their products stay behind it.
+    template <int H>
+    __device__ __forceinline__ void wait_b(Count<H>) {
+      if constexpr (H >= 0)
+        asm volatile("s_waitcnt lgkmcnt(0)"
+                     : "+v"(w[H][0][0]), "+v"(w[H][0][1]), "+v"(w[H][0][2]), "+v"(w[H][0][3]), "+v"(w[H][1][0]),
+                       "+v"(w[H][1][1]), "+v"(w[H][1][2]), "+v"(w[H][1][3]));
+      else
+        wait_lgkm0();
+    }
+    template <int HB, int HA>
+    __device__ __forceinline__ void products(Count<HB>, Count<HA>) {
+      each_of<4>([&](auto bc) LORA_INLINE {
+        constexpr int B = decltype(bc)::value;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          Frag f;
+          f.lo = int4v{w[HB][a][0].x, w[HB][a][0].y, w[HB][a][1].x, w[HB][a][1].y};
+          f.hi = int4v{w[HB][a][2].x, w[HB][a][2].y, w[HB][a][3].x, w[HB][a][3].y};
+          acc[2 * HB + a][4 * HA + B] = stage_product<E, B>(f, fa[B], acc[2 * HB + a][4 * HA + B], sa[HB], sw[HA]);
+        }
+      });
+    }
+  };
+
+  // stages [s0, s1)
+  static __device__ __forceinline__ void run(const NnTile& t, const Scales& sc, int m0, int s0, int s1, char* smem,
+                                             floatx4 (&acc)[4][8]) {
+    using P = Panel<E>;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+      for (int b = 0; b < 8; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (s1 <= s0) return;
+    Loop f{t, sc, acc, smem, t.a, wave >> 2, wave & 3, lane >> 4, lane & 15, lane, wave, s0};
+    const int ar = 8 * wave + (lane >> 3), br = P::RPC * wave + lane / P::CHUNKS;
+    f.aoff = (uint32_t)ar * t.a_row + (uint32_t)(((lane & 7) ^ kc_swz(ar)) << 4);
+    f.boff = (uint32_t)br * t.b_row + (uint32_t)((lane % P::CHUNKS ^ P::swz(br)) << 4);
+#pragma unroll
+    for (int a = 0; a < 2; ++a) f.wa[a] = lds_addr(smem + 256 * 128) + P::read_at(2 * f.wn + a, lane);
+    if constexpr (E::SCALED) {
+      f.rsS = make_rsrc(sc.a, (uint64_t)sc.cells * t.stages * 64);
+      f.soff = scale_words(sc, m0 / 64 + 2 * f.wm, 2, lane);
+      f.bs.load(sc, 0, s0, t.stages, lane);
+    }
+    big_phases<BigBase<E>::CS>(f, s1 - s0, f.wm);
+    formed(acc);
+  }
+};
+
+}  // namespace lora
