@@ -123,26 +123,6 @@ __global__ __launch_bounds__(256) void lora_fp8_dequantize_kernel(const uint8_t*
   *reinterpret_cast<int4v*>(X + (size_t)row * k + 8 * piece) = o;
 }
 
-// Stores a wave's sums as bf16 rows, straight from the registers.
-template <class Core>
-__device__ __forceinline__ void store_tile(const typename Core::Acc& acc, u16* out, int m, int n, int m0, int n0) {
-  constexpr int FA = sizeof(acc) / sizeof(acc[0]), FB = sizeof(acc[0]) / sizeof(acc[0][0]);
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
-#pragma unroll
-  for (int b = 0; b < FB; ++b) {
-    const int row = m0 + Core::row0(wave) + 16 * b + c16;
-#pragma unroll
-    for (int a = 0; a < FA; ++a) {
-      const int col = n0 + Core::col(wave, a) + 4 * g;
-      const floatx4 v = acc[a][b];
-      if (row < m && col < n)
-        *reinterpret_cast<uint2*>(out + (size_t)row * n + col) =
-            uint2{(uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
-                  (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16)};
-    }
-  }
-}
-
 struct Fp8Product {
   const uint8_t *Ac, *As, *Wc, *Ws;
   u16* out;
@@ -163,7 +143,7 @@ __global__ __launch_bounds__(NT) void lora_fp8_fwd_kernel(Fp8Product p) {
   const Scales sc{p.As, p.Ws, (p.m + 63) / 64, nb * blocks, n0 / 128 * blocks, 1, blocks, nb - n0 / 128};
   typename Core::Acc acc;
   Core::run(t, sc, m0, smem, acc);
-  store_tile<Core>(acc, p.out, p.m, p.n, m0, n0);
+  store_tile<Core, BM, BN, NT>(acc, smem, p.out + (size_t)m0 * p.n + n0, (size_t)p.n, p.m - m0, p.n - n0);
 }
 
 template <class Core, int BM, int NT>
@@ -181,10 +161,10 @@ __global__ __launch_bounds__(NT) void lora_fp8_bwd_kernel(Fp8Product p) {
   const int s0 = (int)((int64_t)stages * split / p.splits), s1 = (int)((int64_t)stages * (split + 1) / p.splits);
   Core::run(t, sc, m0, s0, s1, smem, acc);
   if (p.splits == 1) {
-    store_tile<Core>(acc, p.out, p.m, p.k, m0, l0);
+    store_tile<Core, BM, 256, NT>(acc, smem, p.out + (size_t)m0 * p.k + l0, (size_t)p.k, p.m - m0, p.k - l0);
   } else {   // [split][tile][row][column]
     float* to = p.sums + ((size_t)split * tiles + (size_t)tm * p.tiles_n + tn) * BM * 256;
-    constexpr int FA = sizeof(acc) / sizeof(acc[0]), FB = sizeof(acc[0]) / sizeof(acc[0][0]);
+    constexpr int FA = std::extent_v<typename Core::Acc, 0>, FB = std::extent_v<typename Core::Acc, 1>;
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
 #pragma unroll
     for (int b = 0; b < FB; ++b)

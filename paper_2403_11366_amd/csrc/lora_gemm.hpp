@@ -692,4 +692,49 @@ struct NnBig : BigBase<E> {
   }
 };
 
+// ---------------------------------------------------------------------------
+// A tile as bf16 rows in LDS (BM x BN x 2 bytes), 16-byte chunks swizzled by the row,
+// so that it leaves in whole row pieces.
+template <int BN>
+__device__ __forceinline__ uint32_t tile_at(int row, int chunk) {
+  return (uint32_t)(row * (BN * 2) + ((chunk ^ (row & (BN / 8 - 1))) << 4));
+}
+template <class Core, int BN>
+__device__ __forceinline__ void tile_to_lds(const typename Core::Acc& acc, char* smem) {
+  constexpr int FA = std::extent_v<typename Core::Acc, 0>, FB = std::extent_v<typename Core::Acc, 1>;
+  const int lane = lane_fresh(), wave = uniform((int)threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
+#pragma unroll
+  for (int b = 0; b < FB; ++b)
+#pragma unroll
+    for (int a = 0; a < FA; ++a) {
+      const int row = Core::row0(wave) + 16 * b + c16, col = Core::col(wave, a) + 4 * g;
+      const floatx4 v = acc[a][b];
+      *reinterpret_cast<uint2*>(smem + tile_at<BN>(row, col >> 3) + (col & 7) * 2) =
+          uint2{(uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
+                (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16)};
+    }
+}
+// Rows >= nrows and columns >= ncols (a multiple of 8) are not written.
+template <int BM, int BN, int NT>
+__device__ __forceinline__ void lds_to_rows(const char* smem, u16* dst, size_t ld, int nrows, int ncols) {
+  constexpr int CH = BN / 8, STEP = NT / CH;   // rows of a step
+  static_assert(NT % CH == 0 && BM % STEP == 0, "whole steps");
+  const int ch = (int)threadIdx.x % CH, r = (int)threadIdx.x / CH;
+  if (8 * ch >= ncols) return;
+#pragma unroll 8
+  for (int i = 0; i < BM; i += STEP)
+    if (r + i < nrows)
+      *reinterpret_cast<int4v*>(dst + (size_t)(r + i) * ld + 8 * ch) = *reinterpret_cast<const int4v*>(smem + tile_at<BN>(r + i, ch));
+}
+// The tile of a core that has run, stored from its LDS.
+template <class Core, int BM, int BN, int NT>
+__device__ __forceinline__ void store_tile(const typename Core::Acc& acc, char* smem, u16* dst, size_t ld, int nrows,
+                                           int ncols) {
+  static_assert(BM * BN * 2 <= Core::SMEM, "the tile fits the stages");
+  __syncthreads();   // every wave is past its last reads
+  tile_to_lds<Core, BN>(acc, smem);
+  __syncthreads();
+  lds_to_rows<BM, BN, NT>(smem, dst, ld, nrows, ncols);
+}
+
 }  // namespace lora

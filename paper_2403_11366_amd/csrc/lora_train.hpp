@@ -146,8 +146,8 @@ inline XentPlan plan_xent(int64_t rows, int64_t vocab, int64_t k) {
   int64_t most = std::max<int64_t>(1, kPieceElems / p.rows_pad / p.tile_n);
   if (most >= p.vtiles) most = p.vtiles;
   else {
-    const int64_t rounds = most * p.tiles_m / 256;
-    if (rounds > 0) most = std::max<int64_t>(1, rounds * 256 / p.tiles_m);
+    const int64_t rounds = (most * p.tiles_m + p.tiles_m - 1) / 256;
+    if (rounds > 0) most = std::min(most, std::max<int64_t>(1, rounds * 256 / p.tiles_m));
   }
   p.piece_tiles = (int)most;
   p.pieces = (int)cdiv(p.vtiles, most);
@@ -158,27 +158,28 @@ inline XentPlan plan_xent(int64_t rows, int64_t vocab, int64_t k) {
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, p.stages / 8));
   return p;
 }
-// A row's numbers between the kernels.
-struct XentRow {
-  float ref;       // reference of the exponentials, in powers of two
-  float sum;       // of all others but the label's, against it
-  float best;      // largest logit so far (times log2 e), the label's left out
-  float alpha;     // what the sums so far are worth under this piece's reference
-  float zy;        // the label's logit
-  float c1, c2;    // dX = c1 sum_v e_v W_v + c2 W_label
-  int redo;        // the piece's sums are to be added once they are formed again
-};
+// Regions of the workspace.
 struct XentLayout {
-  size_t rows, flags, parts, piece, turned, sums, saved, total;
+  size_t zy;       // [rows_pad] the labels' logits
+  size_t coef;     // [rows_pad][2] dX = c1 sum_v e_v W_v + c2 W_label
+  size_t ref;      // [2][rows_pad] references of the exponentials, of a piece and the next
+  size_t best;     // [2][rows_pad] a piece's largest logits
+  size_t parts;    // [tile][rows_pad] reference and sum of each tile's rows
+  size_t piece;    // [rows_pad][piece] exponentials or gradients of a piece
+  size_t turned;   // [piece][rows_pad] the latter turned, for dW
+  size_t sums;     // [split][tile] fp32 sums of dX
+  size_t saved;    // of the forward, in a call that runs both
+  size_t total;
 };
 inline XentLayout xent_layout(int64_t rows, int64_t vocab, int64_t k, bool dx, bool dw) {
   const XentPlan p = plan_xent(rows, vocab, k);
   XentLayout L;
-  L.rows = 0;
-  L.flags = region((size_t)p.rows_pad * sizeof(XentRow));
-  L.parts = L.flags + region((size_t)p.tiles_m * 4);
-  // maximum and sum of each tile's rows: of all tiles, or of two pieces
-  L.piece = L.parts + region((size_t)std::max(p.vtiles, 2 * p.piece_tiles) * p.rows_pad * 8);
+  L.zy = 0;
+  L.coef = L.zy + region((size_t)p.rows_pad * 4);
+  L.ref = L.coef + region((size_t)p.rows_pad * 8);
+  L.best = L.ref + region((size_t)p.rows_pad * 8);
+  L.parts = L.best + region((size_t)p.rows_pad * 8);
+  L.piece = L.parts + region((size_t)p.vtiles * p.rows_pad * 8);
   L.turned = L.piece + (dx || dw ? region((size_t)(p.rows_pad * p.piece) * 2) : 0);
   L.sums = L.turned + (dw ? region((size_t)(p.rows_pad * p.piece) * 2) : 0);
   L.saved = L.sums + (dx ? region((size_t)p.splits * p.tiles_m * p.tiles_k * p.tile_m * 256 * 4) : 0);

@@ -108,8 +108,8 @@ static int plans() {
         size_t last = 0;
         for (int d = 0; d < 4; ++d) {
           const XentLayout L = xent_layout(rows, vocab, k, d & 1, d >> 1);
-          HOLDS(L.rows <= L.flags && L.flags <= L.parts && L.parts <= L.piece && L.piece <= L.turned && L.turned <= L.sums && L.sums <= L.saved && L.saved <= L.total, rows, vocab, k);
-          HOLDS(L.piece - L.parts >= (size_t)(p.vtiles * p.rows_pad * 8) && L.piece - L.parts >= (size_t)(2 * p.piece_tiles * p.rows_pad * 8), rows, vocab, k);
+          HOLDS(L.coef - L.zy >= (size_t)p.rows_pad * 4 && L.ref - L.coef >= (size_t)p.rows_pad * 8 && L.best - L.ref >= (size_t)p.rows_pad * 8 && L.parts - L.best >= (size_t)p.rows_pad * 8 && L.parts <= L.piece && L.piece <= L.turned && L.turned <= L.sums && L.sums <= L.saved && L.saved <= L.total, rows, vocab, k);
+          HOLDS(L.piece - L.parts >= (size_t)(p.vtiles * p.rows_pad * 8), rows, vocab, k);
           if (d) HOLDS(L.turned - L.piece >= (size_t)(p.rows_pad * p.piece * 2), rows, vocab, k);
           if (d & 2) HOLDS(L.sums - L.turned >= (size_t)(p.rows_pad * p.piece * 2) && L.total - L.saved >= (size_t)(rows * 8), rows, vocab, k);
           if (d & 1) HOLDS(L.saved - L.sums >= (size_t)p.splits * p.rows_pad * p.tiles_k * 256 * 4, rows, vocab, k);
