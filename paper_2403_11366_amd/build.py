@@ -36,9 +36,9 @@ FLAGS = [
 ]
 
 # Workgroups that LDS limits to one wave a SIMD have twice the registers, and the
-# compiler then moves the 4-bit tiles' sums to accumulation registers and back
-# around every product; this keeps them in vector registers.
-SOURCE_FLAGS = {"lora_mx4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# compiler then moves the tiles' sums to accumulation registers and back around
+# every product; this keeps them in vector registers.
+SOURCE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("lora_mx4.hip", "lora_fp8.hip", "lora_xent.hip")}
 
 
 def _compile(src: str) -> str:

@@ -130,6 +130,168 @@ struct Fp8Product {
   int m, n, k, tiles_m, tiles_n, splits;
 };
 
+// ---------------------------------------------------------------------------
+// Few tokens: a workgroup forms 16 FG features x 16 TG tokens with its eight waves on
+// different stages, straight from memory without a barrier until the waves' sums are
+// added, in wave order, through LDS.  A lane loads the two 16-byte chunks of codes
+// that it multiplies; each wave has D stages' loads under way.
+template <int TG, int FG, int D>
+__global__ __launch_bounds__(512) void lora_fp8_few_kernel(Fp8Product p) {
+  constexpr int NW = 8, FR = TG * FG;
+  constexpr int RND = FR < 8 ? FR : 8;   // fragments summed per round
+  __shared__ floatx4 part[NW][RND][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int g = lane >> 4, c = lane & 15;
+  int tm, tn;
+  tile_coords(p.tiles_m, p.tiles_n, 8, (int)blockIdx.x, tm, tn);
+  const int m0 = tm * 16 * TG, n0 = tn * 16 * FG, stages = (p.k + 127) / 128, cells = (p.m + 63) / 64;
+  const uint8_t *wp[FG], *xp[TG], *xsp[TG];   // rows past the matrix: its last one, not stored
+#pragma unroll
+  for (int f = 0; f < FG; ++f) wp[f] = p.Wc + (size_t)min(n0 + 16 * f + c, p.n - 1) * stages * 128 + 16 * g;
+#pragma unroll
+  for (int t = 0; t < TG; ++t) {
+    const int row = min(m0 + 16 * t + c, p.m - 1);
+    xp[t] = p.Ac + (size_t)row * stages * 128 + 16 * g;
+    xsp[t] = p.As + fp8_row_scale_at(row, 0, cells);
+  }
+  const uint8_t* wsp = p.Ws + (size_t)(n0 / 128) * stages;   // (16 FG features share a block)
+  static_assert(128 % (16 * FG) == 0, "a workgroup's features lie in one block of scales");
+  floatx4 acc[FG][TG];
+#pragma unroll
+  for (int f = 0; f < FG; ++f)
+#pragma unroll
+    for (int t = 0; t < TG; ++t) acc[f][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  Frag w[D][FG], x[D][TG];
+  int ws[D], xs[D][TG];
+  auto load = [&](int j, int s) LORA_INLINE {
+#pragma unroll
+    for (int f = 0; f < FG; ++f) {
+      w[j][f].lo = *reinterpret_cast<const int4v*>(wp[f] + (size_t)s * 128);
+      w[j][f].hi = *reinterpret_cast<const int4v*>(wp[f] + (size_t)s * 128 + 64);
+    }
+    ws[j] = wsp[s];
+#pragma unroll
+    for (int t = 0; t < TG; ++t) {
+      x[j][t].lo = *reinterpret_cast<const int4v*>(xp[t] + (size_t)s * 128);
+      x[j][t].hi = *reinterpret_cast<const int4v*>(xp[t] + (size_t)s * 128 + 64);
+      xs[j][t] = xsp[t][(size_t)s * cells * 64];
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < D; ++j)
+    if (wave + NW * j < stages) load(j, wave + NW * j);
+  for (int s0 = wave; s0 < stages; s0 += NW * D) {
+#pragma unroll
+    for (int j = 0; j < D; ++j) {
+      const int s = s0 + NW * j;
+      if (s >= stages) break;
+#pragma unroll
+      for (int t = 0; t < TG; ++t)
+#pragma unroll
+        for (int f = 0; f < FG; ++f) acc[f][t] = stage_product<Fp8, 0>(w[j][f], x[j][t], acc[f][t], ws[j], xs[j][t]);
+      if (s + NW * D < stages) load(j, s + NW * D);
+    }
+  }
+  formed(acc);
+#pragma unroll
+  for (int e0 = 0; e0 < FR; e0 += RND) {
+    if (e0) __syncthreads();
+#pragma unroll
+    for (int e = 0; e < RND; ++e) part[wave][e][lane] = acc[(e0 + e) % FG][(e0 + e) / FG];
+    __syncthreads();
+    if (wave < RND) {
+      floatx4 v = part[0][wave][lane];
+#pragma unroll
+      for (int q = 1; q < NW; ++q) v += part[q][wave][lane];
+      const int e = e0 + wave, f = e % FG, t = e / FG;
+      const int row = m0 + 16 * t + c, col = n0 + 16 * f + 4 * g;
+      if (row < p.m && col < p.n) *reinterpret_cast<uint2*>(p.out + (size_t)row * p.n + col) = bf16x4(v);
+    }
+  }
+}
+
+// Very few values of X: one launch.  Every workgroup quantises X into LDS; its first
+// loads of W are under way meanwhile.  A group of 16 features is formed by KS waves
+// that share its stages, D stages' loads of W ahead; their sums are added in wave
+// order.
+template <int KS, int D>
+__global__ __launch_bounds__(512) void lora_fp8_token_kernel(Fp8Product p, const u16* __restrict__ X) {
+  constexpr int NW = 8;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int stages = (p.k + 127) / 128, m = p.m;
+  char* xc = smem;                                              // [stage][token] rows of 128 bytes, swizzled by the token
+  uint8_t* xs = reinterpret_cast<uint8_t*>(smem + (size_t)stages * m * 128);   // [stage][token]
+  floatx4* part = reinterpret_cast<floatx4*>(smem + (size_t)((stages * m * 129 + 15) & ~15));   // [wave][lane]
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int g = lane >> 4, c = lane & 15;
+  const int grp = (int)blockIdx.x * (NW / KS) + wave / KS, ks = wave % KS, n0 = grp * 16;
+  const uint8_t* wp = p.Wc + (size_t)min(n0 + c, p.n - 1) * stages * 128 + 16 * g;   // rows past the matrix: its last one, not stored
+  const uint8_t* wsp = p.Ws + (size_t)(min(n0, p.n - 1) / 128) * stages;
+  Frag w[D];
+  int ws[D];
+  auto load = [&](int j, int s) LORA_INLINE {
+    w[j].lo = *reinterpret_cast<const int4v*>(wp + (size_t)s * 128);
+    w[j].hi = *reinterpret_cast<const int4v*>(wp + (size_t)s * 128 + 64);
+    ws[j] = wsp[s];
+  };
+#pragma unroll
+  for (int j = 0; j < D; ++j)
+    if (ks + KS * j < stages) load(j, ks + KS * j);
+
+  // X: 16 lanes a token's block.
+  const int pieces = stages * 16, total = m * pieces;
+  const float inv = 1.0f / (float)pieces;
+  for (int e0 = tid; e0 - tid < total; e0 += 512 * 4) {
+    int4v x[4];
+    int row[4], piece[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int e = e0 + 512 * u;
+      row[u] = (int)(((float)e + 0.5f) * inv);   // (below 2^19: at least 0.5 / pieces from a whole number)
+      piece[u] = e - row[u] * pieces;
+      x[u] = e < total && 8 * piece[u] < p.k ? *reinterpret_cast<const int4v*>(X + (size_t)row[u] * p.k + 8 * piece[u])
+                                             : int4v{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (e0 - tid + 512 * u >= total) break;   // (whole blocks of 16 lanes: total is a multiple of 16)
+      const int scale = fp8_scale(max16(top_of(x[u])));
+      const int2w codes = fp8_codes(x[u], scale);
+      if (e0 + 512 * u < total) {
+        const int s = piece[u] >> 4, j = piece[u] & 15, at = s * m + row[u];
+        *reinterpret_cast<int2w*>(xc + at * 128 + (((j >> 1) ^ kc_swz(row[u])) << 4) + (j & 1) * 8) = codes;
+        if (j == 0) xs[at] = (uint8_t)scale;
+      }
+    }
+  }
+  __syncthreads();
+  floatx4 acc{0.f, 0.f, 0.f, 0.f};
+  const int tok = min(c, m - 1);   // (columns past the tokens: the last one's, not stored)
+  const char* xr = xc + tok * 128 + ((g ^ kc_swz(tok)) << 4);
+  const char* xh = xc + tok * 128 + (((4 + g) ^ kc_swz(tok)) << 4);
+  for (int s0 = ks; s0 < stages; s0 += KS * D) {
+#pragma unroll
+    for (int j = 0; j < D; ++j) {
+      const int s = s0 + KS * j;
+      if (s < stages) {
+        const Frag x{*reinterpret_cast<const int4v*>(xr + s * m * 128), *reinterpret_cast<const int4v*>(xh + s * m * 128)};
+        acc = stage_product<Fp8, 0>(w[j], x, acc, ws[j], (int)xs[s * m + tok]);
+        if (s + KS * D < stages) load(j, s + KS * D);
+      }
+    }
+  }
+  asm volatile("" : "+v"(acc));
+  if constexpr (KS > 1) {
+    part[wave * 64 + lane] = acc;
+    __syncthreads();
+    if (ks != 0) return;
+#pragma unroll
+    for (int q = 1; q < KS; ++q) acc += part[(wave + q) * 64 + lane];
+  }
+  const int col = n0 + 4 * g;
+  if (c < m && col < p.n) *reinterpret_cast<uint2*>(p.out + (size_t)c * p.n + col) = bf16x4(acc);
+}
+
 template <class Core, int BM, int BN, int NT>
 __global__ __launch_bounds__(NT) void lora_fp8_fwd_kernel(Fp8Product p) {
   __shared__ __attribute__((aligned(1024))) char smem[Core::SMEM];
@@ -183,10 +345,9 @@ __global__ __launch_bounds__(256) void lora_fp8_join_kernel(const float* __restr
   if (row >= m) return;
   const float* from = sums + ((size_t)(row / 64) * tiles_n + col / 256) * 64 * 256 + (row & 63) * 256 + (col & 255);
   floatx4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const floatx4*>(from + (size_t)s * tiles * 64 * 256);
-  *reinterpret_cast<uint2*>(out + (size_t)row * k + col) =
-      uint2{(uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
-            (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16)};
+  *reinterpret_cast<uint2*>(out + (size_t)row * k + col) = bf16x4(v);
 }
 
 hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, hipStream_t st) {
@@ -222,17 +383,44 @@ static Fp8Product product_of(const Fp8Args& a, const Fp8Layout& L, const Fp8Plan
                     p.splits};
 }
 
+template <class Core, int BM, int BN, int NT>
+static hipError_t run_fwd_tile(const Fp8Plan& p, const Fp8Product& q, hipStream_t st) {
+  hipLaunchKernelGGL((lora_fp8_fwd_kernel<Core, BM, BN, NT>), dim3((unsigned)p.grid), dim3(NT), 0, st, q);
+  return hipGetLastError();
+}
+template <int TG, int D>
+static hipError_t run_few(const Fp8Plan& p, const Fp8Product& q, hipStream_t st) {
+  hipLaunchKernelGGL((lora_fp8_few_kernel<TG, 1, D>), dim3((unsigned)p.grid), dim3(512), 0, st, q);
+  return hipGetLastError();
+}
+template <int KS>
+static hipError_t run_token(const Fp8Plan& p, const Fp8Product& q, const Fp8Args& a, hipStream_t st) {
+  hipLaunchKernelGGL((lora_fp8_token_kernel<KS, 4>), dim3((unsigned)p.grid), dim3(512), fp8_token_lds(a.m, a.k), st, q, a.A);
+  return hipGetLastError();
+}
+
 hipError_t launch_fp8_fwd(const Fp8Args& a, hipStream_t st) {
   const Fp8Layout L = fp8_fwd_layout(a.m, a.n, a.k);
-  const hipError_t e = quantise_input(a, a.k, L, st);
-  if (e != hipSuccess) return e;
   const Fp8Plan p = plan_fp8_fwd(a.m, a.n, a.k);
   const Fp8Product q = product_of(a, L, p);
-  if (p.kind == FP8_BIG)
-    hipLaunchKernelGGL((lora_fp8_fwd_kernel<NtBig<Fp8, false>, 256, 256, 512>), dim3((unsigned)p.grid), dim3(512), 0, st, q);
-  else
-    hipLaunchKernelGGL((lora_fp8_fwd_kernel<NtCore<Fp8, 64, 128, 1, 4, 3, false>, 64, 128, 256>), dim3((unsigned)p.grid),
-                       dim3(256), 0, st, q);
+  if (p.kind == FP8_TOKEN_8) return run_token<8>(p, q, a, st);
+  if (p.kind == FP8_TOKEN_2) return run_token<2>(p, q, a, st);
+  const hipError_t e = quantise_input(a, a.k, L, st);
+  if (e != hipSuccess) return e;
+  switch (p.kind) {
+    case FP8_FEW_1: return run_few<1, 4>(p, q, st);
+    case FP8_FEW_2: return run_few<2, 2>(p, q, st);
+    case FP8_64x64: return run_fwd_tile<NtCore<Fp8, 64, 64, 1, 4, 4, false>, 64, 64, 256>(p, q, st);
+    case FP8_64x128: return run_fwd_tile<NtCore<Fp8, 64, 128, 1, 4, 3, false>, 64, 128, 256>(p, q, st);
+    case FP8_128x128: return run_fwd_tile<NtCore<Fp8, 128, 128, 2, 4, 3, false>, 128, 128, 512>(p, q, st);
+    case FP8_256x128: return run_fwd_tile<NtCore<Fp8, 256, 128, 4, 2, 3, false>, 256, 128, 512>(p, q, st);
+    default: return run_fwd_tile<NtBig<Fp8, false>, 256, 256, 512>(p, q, st);
+  }
+}
+
+template <class Core, int BM, int NT>
+static hipError_t run_bwd_tile(const Fp8Plan& p, const Fp8Product& q, hipStream_t st) {
+  hipLaunchKernelGGL((lora_fp8_bwd_kernel<Core, BM, NT>), dim3((unsigned)p.grid), dim3(NT), 0, st, q);
   return hipGetLastError();
 }
 
@@ -242,12 +430,11 @@ hipError_t launch_fp8_bwd(const Fp8Args& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const Fp8Plan p = plan_fp8_bwd(a.m, a.n, a.k);
   const Fp8Product q = product_of(a, L, p);
-  if (p.kind == FP8_BIG)
-    hipLaunchKernelGGL((lora_fp8_bwd_kernel<NnBig<Fp8>, 256, 512>), dim3((unsigned)p.grid), dim3(512), 0, st, q);
-  else
-    hipLaunchKernelGGL((lora_fp8_bwd_kernel<NnCore<Fp8, 64, 256, 4, 3>, 64, 256>), dim3((unsigned)p.grid), dim3(256), 0,
-                       st, q);
-  e = hipGetLastError();
+  switch (p.kind) {
+    case FP8_BACK_64x256: e = run_bwd_tile<NnCore<Fp8, 64, 256, 1, 4, 3>, 64, 256>(p, q, st); break;
+    case FP8_BACK_128x256: e = run_bwd_tile<NnCore<Fp8, 128, 256, 2, 4, 3>, 128, 512>(p, q, st); break;
+    default: e = run_bwd_tile<NnBig<Fp8>, 256, 512>(p, q, st); break;
+  }
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL(lora_fp8_join_kernel, dim3((unsigned)cdiv(a.m * (a.k / 4), 256)), dim3(256), 0, st, q.sums, a.out,
                      (int)a.m, (int)a.k, p.tiles_n, p.tiles_m * p.tiles_n, p.splits);

@@ -50,6 +50,11 @@ struct Fp8 {   // e4m3
   static constexpr bool SCALED = true;
 };
 
+__device__ __forceinline__ uint2 bf16x4(const floatx4& v) {
+  return uint2{(uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
+               (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16)};
+}
+
 struct Frag {   // of 16 rows (or columns) x a stage
   int4v lo, hi;
 };
@@ -113,13 +118,24 @@ struct NnTile {
   uint64_t b_bytes;               // from b to the operand's end
   int stages;
 };
-// B's rows of stage kb: what is left of the operand, at most a stage of rows.
-template <class E>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t nn_rows(const NnTile& t, int kb) {
-  const uint64_t at = (uint64_t)kb * E::KS * t.b_row;
-  const uint64_t left = t.b_bytes > at ? t.b_bytes - at : 0, most = (uint64_t)E::KS * t.b_row;
-  return make_rsrc(t.b + (left ? at : 0), left < most ? left : most);
-}
+// B's rows from the current stage on: what is left of the operand (past its end
+// nothing, and copies of zeros).
+struct NnRows {
+  const char* at;
+  uint64_t left;
+  uint32_t step;   // bytes of a stage's rows
+  __device__ __forceinline__ void start(const NnTile& t, int stage, int ks) {
+    step = t.b_row * (uint32_t)ks;
+    const uint64_t skip = (uint64_t)stage * step;
+    left = t.b_bytes > skip ? t.b_bytes - skip : 0;
+    at = t.b + (left ? skip : 0);
+  }
+  __device__ __forceinline__ void next() {
+    at += step;
+    left = left > step ? left - step : 0;
+  }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows() const { return make_rsrc(at, left); }
+};
 
 // The weight's scale bytes of up to 64 stages in one register, a stage to a lane
 // (with two column blocks a stage: 32 stages, two lanes each).
@@ -140,13 +156,18 @@ struct BScales {
 
 // ---------------------------------------------------------------------------
 // C = A B^T, BM x BN by WM x WN waves, NS stages of LDS copied from memory straight
-// into LDS, one barrier a stage.
+// into LDS, one barrier a stage, fragments read a stage ahead.
+//
+// A compute unit often holds one such workgroup, a wave to a SIMD, and then the wave's
+// own instructions bound a stage: the loop is unrolled over the stages' places, whose
+// addresses are constants, and copies past the end take the last stage again (nobody
+// reads them) instead of a condition each.
 template <class E, int BM, int BN, int WM, int WN, int NS, bool TAIL>
 struct NtCore {
   static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FA = TN / 16, FB = TM / 16;
   static constexpr int CX = BM / 8 / NW, CB = BN / 8 / NW, CS = E::SCALED ? 1 : 0, C = CX + CB + CS;
   static constexpr int SOFF = (BM + BN) * 128, STAGE = SOFF + CS * NW * 256, SMEM = NS * STAGE;
-  static_assert(TM % 64 == 0 && TN % 16 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (NS - 1) * C < 64, "tile");
+  static_assert(TM % 64 == 0 && TN % 16 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NS * C < 64, "tile");
   typedef floatx4 Acc[FA][FB];
   static __device__ __forceinline__ int row0(int wave) { return wave / WN * TM; }
   static __device__ __forceinline__ int col(int wave, int a) { return wave % WN * TN + 16 * a; }
@@ -160,58 +181,83 @@ struct NtCore {
       for (int b = 0; b < FB; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
     const int crow = 8 * wave;
     const uint32_t kcol = (uint32_t)(((lane & 7) ^ kc_swz(crow + l8)) << 4);
-    const uint32_t aoff = (uint32_t)(crow + l8) * t.a_row + kcol, boff = (uint32_t)(crow + l8) * t.b_row + kcol;
+    uint32_t aoff[CX], boff[CB], soff = kOOB;
+#pragma unroll
+    for (int i = 0; i < CX; ++i) aoff[i] = (uint32_t)(crow + l8 + 8 * NW * i) * t.a_row + kcol;
+#pragma unroll
+    for (int i = 0; i < CB; ++i) boff[i] = (uint32_t)(crow + l8 + 8 * NW * i) * t.b_row + kcol;
     __amdgpu_buffer_rsrc_t rsS = t.a;
-    uint32_t soff = kOOB;
     BScales<1> bs;
     const int bcol = wn * TN / 128;
+    const uint32_t sstep = E::SCALED ? (uint32_t)sc.cells * 64 : 0;
     if constexpr (E::SCALED) {
-      rsS = make_rsrc(sc.a, (uint64_t)sc.cells * t.stages * 64);
+      rsS = make_rsrc(sc.a, (uint64_t)sstep * t.stages);
       soff = scale_words(sc, m0 / 64 + wm * (TM / 64), TM / 64, lane);
+      bs.load(sc, bcol, 0, t.stages, lane);
     }
-    auto copy = [&](int kb) LORA_INLINE {   // past the last stage: zeros, so that the counts hold
-      char* sb = smem + kb % NS * STAGE;
-      const bool live = kb < t.stages;
-      const uint32_t at = live ? (uint32_t)kb * 128 : 0u;
-      const bool in = live && (!TAIL || at + kcol < t.kbytes);
+    const uint32_t last = (uint32_t)(t.stages - 1) * 128, slast = (uint32_t)(t.stages - 1) * sstep;
+    uint32_t at = 0, sat = 0;   // of the next stage to copy
+    char* const mine = smem + crow * 128;
+    auto copy = [&](auto place) LORA_INLINE {
+      char* sb = mine + decltype(place)::value * STAGE;
+      const bool out = TAIL && at + kcol >= t.kbytes;
 #pragma unroll
-      for (int i = 0; i < CX; ++i)
-        dma16(t.a, in ? aoff + (uint32_t)(8 * NW * i) * t.a_row : kOOB, at, sb + (crow + 8 * NW * i) * 128);
+      for (int i = 0; i < CX; ++i) dma16(t.a, out ? kOOB : aoff[i], at, sb + 8 * NW * i * 128);
 #pragma unroll
-      for (int i = 0; i < CB; ++i)
-        dma16(t.b, in ? boff + (uint32_t)(8 * NW * i) * t.b_row : kOOB, at, sb + (BM + crow + 8 * NW * i) * 128);
-      if constexpr (E::SCALED)
-        dma4(rsS, live ? soff : kOOB, live ? (uint32_t)kb * sc.cells * 64 : 0u, sb + SOFF + wave * 256);
-    };
-    if constexpr (E::SCALED) bs.load(sc, bcol, 0, t.stages, lane);
-#pragma unroll
-    for (int j = 0; j < NS - 1; ++j) copy(j);
-    for (int kb = 0; kb < t.stages; ++kb) {
-      if constexpr (E::SCALED)
-        if (kb - bs.base == bs.SPAN) bs.load(sc, bcol, kb, t.stages, lane);
-      copy_barrier<(NS - 2) * C>();   // this stage has landed, and every wave has read the one before
-      copy(kb + NS - 1);
-      const char* sb = smem + kb % NS * STAGE;
-      int sa = 0, sw[TM / 64] = {};
+      for (int i = 0; i < CB; ++i) dma16(t.b, out ? kOOB : boff[i], at, sb + (BM + 8 * NW * i) * 128);
       if constexpr (E::SCALED) {
-        sa = bs.at(kb, 0);
-#pragma unroll
-        for (int i = 0; i < TM / 64; ++i)
-          sw[i] = *reinterpret_cast<const int*>(sb + SOFF + wave * 256 + i * 64 + c16 * 4);
+        dma4(rsS, soff, sat, smem + decltype(place)::value * STAGE + SOFF + wave * 256);
+        sat = min(sat + sstep, slast);
       }
-      Frag fa[FA];
+      at = min(at + 128, last);
+    };
+    Frag fa[2][FA], fb[2][FB];   // of this stage and the next
+    int sa[2] = {}, sw[2][TM / 64] = {};
+    // Rows 16 apart swizzle alike, and the second chunk is 4 further.
+    const uint32_t f0 = kc_offset(c16, g), f1 = f0 ^ 64;
+    const char *a0 = smem + (BM + wn * TN) * 128 + f0, *a1 = smem + (BM + wn * TN) * 128 + f1;
+    const char *b0 = smem + wm * TM * 128 + f0, *b1 = smem + wm * TM * 128 + f1;
+    const char* s0 = smem + SOFF + wave * 256 + c16 * 4;
+    auto read = [&](int kb, auto place, auto set) LORA_INLINE {
+      constexpr int S = decltype(set)::value, O = decltype(place)::value * STAGE;
+      if constexpr (E::SCALED) {
+        sa[S] = bs.at(kb, 0);
 #pragma unroll
-      for (int a = 0; a < FA; ++a) {
-        fa[a].lo = __builtin_bit_cast(int4v, kc_read(sb + BM * 128, wn * TN + 16 * a + c16, g));
-        fa[a].hi = __builtin_bit_cast(int4v, kc_read(sb + BM * 128, wn * TN + 16 * a + c16, 4 + g));
+        for (int i = 0; i < TM / 64; ++i) sw[S][i] = *reinterpret_cast<const int*>(s0 + O + i * 64);
       }
+#pragma unroll
+      for (int a = 0; a < FA; ++a)
+        fa[S][a] = Frag{*reinterpret_cast<const int4v*>(a0 + O + 2048 * a), *reinterpret_cast<const int4v*>(a1 + O + 2048 * a)};
+#pragma unroll
+      for (int b = 0; b < FB; ++b)
+        fb[S][b] = Frag{*reinterpret_cast<const int4v*>(b0 + O + 2048 * b), *reinterpret_cast<const int4v*>(b1 + O + 2048 * b)};
+    };
+    auto multiply = [&](auto set) LORA_INLINE {
+      constexpr int S = decltype(set)::value;
       each_of<FB>([&](auto bc) LORA_INLINE {
         constexpr int B = decltype(bc)::value;
-        Frag fb;
-        fb.lo = __builtin_bit_cast(int4v, kc_read(sb, wm * TM + 16 * B + c16, g));
-        fb.hi = __builtin_bit_cast(int4v, kc_read(sb, wm * TM + 16 * B + c16, 4 + g));
 #pragma unroll
-        for (int a = 0; a < FA; ++a) acc[a][B] = stage_product<E, B & 3>(fa[a], fb, acc[a][B], sa, sw[B >> 2]);
+        for (int a = 0; a < FA; ++a)
+          acc[a][B] = stage_product<E, B & 3>(fa[S][a], fb[S][B], acc[a][B], sa[S], sw[S][B >> 2]);
+      });
+    };
+    each_of<NS>([&](auto j) LORA_INLINE { copy(j); });
+    copy_barrier<(NS - 1) * C>();
+    read(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+    constexpr int U = NS % 2 ? 2 * NS : NS;
+    for (int k0 = 0; k0 < t.stages; k0 += U) {
+      if constexpr (E::SCALED)
+        if (k0 + U - bs.base >= bs.SPAN) bs.load(sc, bcol, k0, t.stages, lane);   // (U and the next stage's)
+      each_of<U>([&](auto jc) LORA_INLINE {
+        constexpr int J = decltype(jc)::value;
+        // The next stage has landed, and every wave has read this one, whose place is
+        // filled again; the next one's fragments are read under this one's products.
+        if (J == 0 || k0 + J < t.stages) {
+          copy_barrier<(NS - 2) * C>();
+          copy(std::integral_constant<int, J % NS>{});
+          read(k0 + J + 1, std::integral_constant<int, (J + 1) % NS>{}, std::integral_constant<int, (J + 1) & 1>{});
+          multiply(std::integral_constant<int, J & 1>{});
+        }
       });
     }
     formed(acc);
@@ -255,112 +301,137 @@ struct Panel {
   }
 };
 
-// C = A B, BM x BN (BN 128 or 256) by WN waves along the columns, NS stages.
-template <class E, int BM, int BN, int WN, int NS>
+// C = A B, BM x BN (BN 128 or 256) by WM x WN waves, NS stages.
+template <class E, int BM, int BN, int WM, int WN, int NS>
 struct NnCore {
-  static constexpr int NW = WN, TN = BN / WN, FA = TN / 16, FB = BM / 16;
+  static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FA = TN / 16, FB = TM / 16;
   static constexpr int CX = BM / 8 / NW, CB = BN * 128 / 1024 / NW, CS = E::SCALED ? 1 : 0, C = CX + CB + CS;
   static constexpr int SOFF = (BM + BN) * 128, STAGE = SOFF + CS * NW * 256, SMEM = NS * STAGE;
-  static_assert(BM == 64 && BN % 128 == 0 && TN % 16 == 0 && 128 % TN == 0 && (NS - 1) * C < 64, "tile");
+  static_assert(TM == 64 && BN % 128 == 0 && TN % 16 == 0 && 128 % TN == 0 && NS * C < 64, "tile");
   typedef floatx4 Acc[FA][FB];
-  static __device__ __forceinline__ int row0(int) { return 0; }
-  static __device__ __forceinline__ int col(int wave, int a) { return wave * TN + 16 * a; }
+  static __device__ __forceinline__ int row0(int wave) { return wave / WN * TM; }
+  static __device__ __forceinline__ int col(int wave, int a) { return wave % WN * TN + 16 * a; }
 
   // stages [s0, s1) of the contraction
   static __device__ __forceinline__ void run(const NnTile& t, const Scales& sc, int m0, int s0, int s1, char* smem,
                                              Acc& acc) {
     using P = Panel<E>;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int g = lane >> 4, c16 = lane & 15, l8 = lane >> 3;
+    const int wm = wave / WN, wn = wave % WN, g = lane >> 4, c16 = lane & 15, l8 = lane >> 3;
 #pragma unroll
     for (int a = 0; a < FA; ++a)
 #pragma unroll
       for (int b = 0; b < FB; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (s1 <= s0) return;
     const int crow = 8 * wave;
     const uint32_t kcol = (uint32_t)(((lane & 7) ^ kc_swz(crow + l8)) << 4);
-    const uint32_t aoff = (uint32_t)(crow + l8) * t.a_row + kcol;
-    __amdgpu_buffer_rsrc_t rsS = t.a;
-    uint32_t soff = kOOB;
-    BScales<1> bs;
-    const int bcol = wave * TN / 128;
-    if constexpr (E::SCALED) {
-      rsS = make_rsrc(sc.a, (uint64_t)sc.cells * t.stages * 64);
-      soff = scale_words(sc, m0 / 64, BM / 64, lane);
+    uint32_t aoff[CX], boff[CB], soff = kOOB;
+#pragma unroll
+    for (int i = 0; i < CX; ++i) aoff[i] = (uint32_t)(crow + l8 + 8 * NW * i) * t.a_row + kcol;
+#pragma unroll
+    for (int i = 0; i < CB; ++i) {
+      const int q = wave + NW * i, p = q >> 4, row = (q & 15) * P::RPC + lane / P::CHUNKS;   // 16 copies a panel
+      boff[i] = (uint32_t)row * t.b_row + (uint32_t)(p * P::ROW + 16 * (lane % P::CHUNKS ^ P::swz(row)));
     }
-    auto copy = [&](int kb) LORA_INLINE {
-      char* sb = smem + (kb - s0) % NS * STAGE;
-      const bool live = kb < s1;
-      const uint32_t at = live ? (uint32_t)kb * 128 : 0u;
+    __amdgpu_buffer_rsrc_t rsS = t.a;
+    BScales<1> bs;
+    const int bcol = wn * TN / 128;
+    const uint32_t sstep = E::SCALED ? (uint32_t)sc.cells * 64 : 0;
+    if constexpr (E::SCALED) {
+      rsS = make_rsrc(sc.a, (uint64_t)sstep * t.stages);
+      soff = scale_words(sc, m0 / 64 + wm, 1, lane);
+      bs.load(sc, bcol, s0, t.stages, lane);
+    }
+    const uint32_t last = (uint32_t)(s1 - 1) * 128, slast = (uint32_t)(s1 - 1) * sstep;
+    uint32_t at = (uint32_t)s0 * 128, sat = (uint32_t)s0 * sstep;   // of the next stage to copy
+    NnRows rows;
+    rows.start(t, s0, E::KS);
+    auto copy = [&](auto place) LORA_INLINE {
+      char* sb = smem + decltype(place)::value * STAGE;
 #pragma unroll
-      for (int i = 0; i < CX; ++i)
-        dma16(t.a, live ? aoff + (uint32_t)(8 * NW * i) * t.a_row : kOOB, at, sb + (crow + 8 * NW * i) * 128);
-      const __amdgpu_buffer_rsrc_t rsB = nn_rows<E>(t, live ? kb : s0);
+      for (int i = 0; i < CX; ++i) dma16(t.a, aoff[i], at, sb + (crow + 8 * NW * i) * 128);
+      const __amdgpu_buffer_rsrc_t rs = rows.rows();
 #pragma unroll
-      for (int i = 0; i < CB; ++i) {
-        const int q = wave + NW * i, p = q >> 4, row = (q & 15) * P::RPC + lane / P::CHUNKS;   // 16 copies a panel
-        const int ch = lane % P::CHUNKS ^ P::swz(row);
-        dma16(rsB, live ? (uint32_t)row * t.b_row + (uint32_t)(p * P::ROW + 16 * ch) : kOOB, 0,
-              sb + BM * 128 + q * 1024);
+      for (int i = 0; i < CB; ++i) dma16(rs, boff[i], 0, sb + BM * 128 + (wave + NW * i) * 1024);
+      if constexpr (E::SCALED) {
+        dma4(rsS, soff, sat, sb + SOFF + wave * 256);
+        sat = min(sat + sstep, slast);
       }
-      if constexpr (E::SCALED)
-        dma4(rsS, live ? soff : kOOB, live ? (uint32_t)kb * sc.cells * 64 : 0u, sb + SOFF + wave * 256);
+      at = min(at + 128, last);
+      rows.next();
     };
-    if constexpr (E::SCALED) bs.load(sc, bcol, s0, t.stages, lane);
     uint32_t wa[FA];
 #pragma unroll
     for (int a = 0; a < FA; ++a) {
-      const int f = (wave * TN + 16 * a) / 16;
+      const int f = (wn * TN + 16 * a) / 16;
       wa[a] = lds_addr(smem + BM * 128 + (f >> 3) * 16384) + P::read_at(f & 7, lane);
     }
-#pragma unroll
-    for (int j = 0; j < NS - 1; ++j) copy(s0 + j);
-    for (int kb = s0; kb < s1; ++kb) {
-      if constexpr (E::SCALED)
-        if (kb - bs.base == bs.SPAN) bs.load(sc, bcol, kb, t.stages, lane);
-      copy_barrier<(NS - 2) * C>();
-      copy(kb + NS - 1);
-      const int here = (kb - s0) % NS * STAGE;
-      const char* sb = smem + here;
-      int sa = 0, sw = 0;
+    Frag fb[2][FB];              // of this stage and the next
+    int2w w[2][FA][4];
+    int sa[2] = {}, sw[2] = {};
+    static_assert(FA == 4, "the wait's operands");
+    const uint32_t f0 = kc_offset(c16, g), f1 = f0 ^ 64;
+    const char *b0 = smem + wm * TM * 128 + f0, *b1 = smem + wm * TM * 128 + f1;
+    auto read = [&](int kb, auto place, auto set) LORA_INLINE {
+      constexpr int S = decltype(set)::value, O = decltype(place)::value * STAGE;
       if constexpr (E::SCALED) {
-        sa = bs.at(kb, 0);
-        sw = *reinterpret_cast<const int*>(sb + SOFF + wave * 256 + c16 * 4);
+        sa[S] = bs.at(kb, 0);
+        sw[S] = *reinterpret_cast<const int*>(smem + O + SOFF + wave * 256 + c16 * 4);
       }
-      Frag fb[FB];
 #pragma unroll
-      for (int b = 0; b < FB; ++b) {
-        fb[b].lo = __builtin_bit_cast(int4v, kc_read(sb, 16 * b + c16, g));
-        fb[b].hi = __builtin_bit_cast(int4v, kc_read(sb, 16 * b + c16, 4 + g));
-      }
+      for (int b = 0; b < FB; ++b)
+        fb[S][b] = Frag{*reinterpret_cast<const int4v*>(b0 + O + 2048 * b), *reinterpret_cast<const int4v*>(b1 + O + 2048 * b)};
       __builtin_amdgcn_sched_barrier(0);
-      int2w w[FA][4];
 #pragma unroll
       for (int a = 0; a < FA; ++a) {
-        const uint32_t at = wa[a] + (uint32_t)here;
-        read_tr_asm<E, 0>(w[a][0], at);
-        read_tr_asm<E, 1024>(w[a][1], at);
-        read_tr_asm<E, 8192>(w[a][2], at);
-        read_tr_asm<E, 9216>(w[a][3], at);
+        const uint32_t from = wa[a] + (uint32_t)O;
+        read_tr_asm<E, 0>(w[S][a][0], from);
+        read_tr_asm<E, 1024>(w[S][a][1], from);
+        read_tr_asm<E, 8192>(w[S][a][2], from);
+        read_tr_asm<E, 9216>(w[S][a][3], from);
       }
-      if constexpr (FA == 4)
-        asm volatile("s_waitcnt lgkmcnt(0)"
-                     : "+v"(w[0][0]), "+v"(w[0][1]), "+v"(w[0][2]), "+v"(w[0][3]), "+v"(w[1][0]), "+v"(w[1][1]),
-                       "+v"(w[1][2]), "+v"(w[1][3]), "+v"(w[2][0]), "+v"(w[2][1]), "+v"(w[2][2]), "+v"(w[2][3]),
-                       "+v"(w[3][0]), "+v"(w[3][1]), "+v"(w[3][2]), "+v"(w[3][3]));
-      else
-        asm volatile("s_waitcnt lgkmcnt(0)"
-                     : "+v"(w[0][0]), "+v"(w[0][1]), "+v"(w[0][2]), "+v"(w[0][3]), "+v"(w[1][0]), "+v"(w[1][1]),
-                       "+v"(w[1][2]), "+v"(w[1][3]));
-      static_assert(FA == 4 || FA == 2, "the wait's operands");
+    };
+    auto arrived = [&](auto set) LORA_INLINE {   // (before any branch)
+      constexpr int S = decltype(set)::value;
+      asm volatile("s_waitcnt lgkmcnt(0)"
+                   : "+v"(w[S][0][0]), "+v"(w[S][0][1]), "+v"(w[S][0][2]), "+v"(w[S][0][3]), "+v"(w[S][1][0]),
+                     "+v"(w[S][1][1]), "+v"(w[S][1][2]), "+v"(w[S][1][3]), "+v"(w[S][2][0]), "+v"(w[S][2][1]),
+                     "+v"(w[S][2][2]), "+v"(w[S][2][3]), "+v"(w[S][3][0]), "+v"(w[S][3][1]), "+v"(w[S][3][2]),
+                     "+v"(w[S][3][3]));
       __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](auto set) LORA_INLINE {
+      constexpr int S = decltype(set)::value;
       each_of<FB>([&](auto bc) LORA_INLINE {
         constexpr int B = decltype(bc)::value;
 #pragma unroll
         for (int a = 0; a < FA; ++a) {
           Frag f;
-          f.lo = int4v{w[a][0].x, w[a][0].y, w[a][1].x, w[a][1].y};
-          f.hi = int4v{w[a][2].x, w[a][2].y, w[a][3].x, w[a][3].y};
-          acc[a][B] = stage_product<E, B & 3>(f, fb[B], acc[a][B], sa, sw);
+          f.lo = int4v{w[S][a][0].x, w[S][a][0].y, w[S][a][1].x, w[S][a][1].y};
+          f.hi = int4v{w[S][a][2].x, w[S][a][2].y, w[S][a][3].x, w[S][a][3].y};
+          acc[a][B] = stage_product<E, B & 3>(f, fb[S][B], acc[a][B], sa[S], sw[S]);
+        }
+      });
+    };
+    using I0 = std::integral_constant<int, 0>;
+    each_of<NS>([&](auto j) LORA_INLINE { copy(j); });
+    copy_barrier<(NS - 1) * C>();
+    read(s0, I0{}, I0{});
+    arrived(I0{});
+    constexpr int U = NS % 2 ? 2 * NS : NS;
+    for (int k0 = s0; k0 < s1; k0 += U) {
+      if constexpr (E::SCALED)
+        if (k0 + U - bs.base >= bs.SPAN) bs.load(sc, bcol, k0, t.stages, lane);
+      each_of<U>([&](auto jc) LORA_INLINE {   // as in NtCore
+        constexpr int J = decltype(jc)::value;
+        using Next = std::integral_constant<int, (J + 1) & 1>;
+        if (J == 0 || k0 + J < s1) {
+          copy_barrier<(NS - 2) * C>();
+          copy(std::integral_constant<int, J % NS>{});
+          read(k0 + J + 1, std::integral_constant<int, (J + 1) % NS>{}, Next{});
+          multiply(std::integral_constant<int, J & 1>{});
+          __builtin_amdgcn_sched_barrier(0);
+          arrived(Next{});
         }
       });
     }
@@ -584,8 +655,9 @@ struct NnBig : BigBase<E> {
     char* smem;
     __amdgpu_buffer_rsrc_t rsS;
     int wm, wn, g, c16, lane, wave, s0;   // s0: the first stage of the contraction
-    uint32_t aoff, boff, soff;
+    uint32_t aoff, boff[2], soff;
     uint32_t wa[2];
+    NnRows rows;
     Frag fa[4];
     int2w w[2][2][4];                // B halves: [half][fragment][read]
     int sw[2], sa[2];
@@ -609,10 +681,10 @@ struct NnBig : BigBase<E> {
     }
     __device__ __forceinline__ void copy_b(int kb, int h) {
       char* sb = smem + (kb & 1) * kBigStage + 256 * 128 + h * 16384 + wave * 1024;
-      const __amdgpu_buffer_rsrc_t rs = nn_rows<E>(t, s0 + kb);
+      const __amdgpu_buffer_rsrc_t rs = rows.rows();   // (a stage's halves are copied in order, stage by stage)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        dma16(rs, boff + (uint32_t)(8 * P::RPC * i) * t.b_row + (uint32_t)(h * P::ROW), 0, sb + i * 8192);
+      for (int i = 0; i < 2; ++i) dma16(rs, boff[i] + (uint32_t)(h * P::ROW), 0, sb + i * 8192);
+      if (h == 1) rows.next();
     }
     __device__ __forceinline__ void read_a(int kb, int h) {
       const char* As = smem + (kb & 1) * kBigStage;
@@ -679,7 +751,10 @@ struct NnBig : BigBase<E> {
     Loop f{t, sc, acc, smem, t.a, wave >> 2, wave & 3, lane >> 4, lane & 15, lane, wave, s0};
     const int ar = 8 * wave + (lane >> 3), br = P::RPC * wave + lane / P::CHUNKS;
     f.aoff = (uint32_t)ar * t.a_row + (uint32_t)(((lane & 7) ^ kc_swz(ar)) << 4);
-    f.boff = (uint32_t)br * t.b_row + (uint32_t)((lane % P::CHUNKS ^ P::swz(br)) << 4);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      f.boff[i] = (uint32_t)(br + 8 * P::RPC * i) * t.b_row + (uint32_t)((lane % P::CHUNKS ^ P::swz(br)) << 4);
+    f.rows.start(t, s0, E::KS);
 #pragma unroll
     for (int a = 0; a < 2; ++a) f.wa[a] = lds_addr(smem + 256 * 128) + P::read_at(2 * f.wn + a, lane);
     if constexpr (E::SCALED) {
@@ -708,10 +783,7 @@ __device__ __forceinline__ void tile_to_lds(const typename Core::Acc& acc, char*
 #pragma unroll
     for (int a = 0; a < FA; ++a) {
       const int row = Core::row0(wave) + 16 * b + c16, col = Core::col(wave, a) + 4 * g;
-      const floatx4 v = acc[a][b];
-      *reinterpret_cast<uint2*>(smem + tile_at<BN>(row, col >> 3) + (col & 7) * 2) =
-          uint2{(uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
-                (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16)};
+      *reinterpret_cast<uint2*>(smem + tile_at<BN>(row, col >> 3) + (col & 7) * 2) = bf16x4(acc[a][b]);
     }
 }
 // Rows >= nrows and columns >= ncols (a multiple of 8) are not written.

@@ -57,31 +57,117 @@ struct Fp8Args {
   int64_t m, n, k;   // W is [n, k]
 };
 
-enum Fp8Kind { FP8_SMALL, FP8_BIG };
+// Kernels of the forward: one launch that quantises X on its way for very few values
+// of it; else X is quantised before, and the product is formed by waves on different
+// stages straight from memory (few tokens) or by tiles staged in LDS.  The backward
+// has tiles alone, whose contraction workgroups may share.
+enum Fp8Kind { FP8_TOKEN_8, FP8_TOKEN_2, FP8_FEW_1, FP8_FEW_2, FP8_64x64, FP8_64x128, FP8_128x128, FP8_256x128, FP8_256x256 };
+enum Fp8BackKind { FP8_BACK_64x256, FP8_BACK_128x256, FP8_BACK_256x256 };
+
 struct Fp8Plan {
-  Fp8Kind kind;
-  int tiles_m, tiles_n, splits;
+  int kind;               // of the forward's or the backward's
+  int tiles_m, tiles_n;   // of the output
+  int splits;             // workgroups that share a tile's contraction
   int64_t grid;
+  int block;
 };
-inline Fp8Plan plan_fp8_fwd(int64_t m, int64_t n, int64_t k) {
-  (void)k;
+
+// Tiles are chosen by their estimated time in us, launches and the quantisation left
+// out: a round of workgroups that fills the compute units takes c + full x stages, one
+// of few of them c + light x stages, the last one in between.
+//   Forward, fitted to k = 2048 to 11008 (us): 64 x 4096 x 4096 9.9 on 64 x 64 (14.6 on
+// 64 x 128, 15.0 from memory), 24 x 32000 x 4096 21.8 on both, 128 x 11008 x 4096 18.2
+// on 64 x 128 (21 on 64 x 64), 1024 x 4096 x 4096 22.4 on 128 x 128 (28 on 64 x 128, 32
+// on 256 x 128), 1531 x 4104 x 3208 26.7 on 256 x 128 (32 on 128 x 128, 35 on 256 x
+// 256), 4096 x 4096 x 4096 53 on 256 x 256 (69 on 256 x 128).
+//   Backward: 200 x 4096 x 4096 25 on 64 x 256, 17 with four workgroups to a tile, 1024
+// x 4096 x 4096 28.5 on 64 x 256 (35 on 128 x 256, 43 on 256 x 256), 2048 x 4096 x 4096
+// 37 on 128 x 256 (47, 55), 1024 x 4096 x 11008 49 on 256 x 256 (68 on 128 x 256).
+struct TileCost {
+  int kind, bm, bn, block;
+  double c, light, full;
+};
+constexpr TileCost kFp8Tiles[5] = {{FP8_64x64, 64, 64, 256, 1.5, 0.26, 0.29},
+                                   {FP8_64x128, 64, 128, 256, 1.8, 0.40, 0.42},
+                                   {FP8_128x128, 128, 128, 512, 2.5, 0.49, 0.62},
+                                   {FP8_256x128, 256, 128, 512, 4.0, 0.77, 1.00},
+                                   {FP8_256x256, 256, 256, 512, 6.0, 1.03, 1.45}};
+constexpr TileCost kFp8BackTiles[3] = {{FP8_BACK_64x256, 64, 256, 256, 2.5, 0.71, 0.80},
+                                       {FP8_BACK_128x256, 128, 256, 512, 3.5, 0.80, 1.02},
+                                       {FP8_BACK_256x256, 256, 256, 512, 6.0, 1.03, 1.65}};
+inline double tile_time(const TileCost& t, int64_t grid, double stages) {
+  const int64_t rounds = cdiv(grid, 256), last = grid - (rounds - 1) * 256;
+  return (double)(rounds - 1) * (t.c + t.full * stages) + t.c + (t.light + (t.full - t.light) * (double)last / 256) * stages;
+}
+inline Fp8Plan fp8_plan_of(int kind, int64_t rows, int64_t cols, int bm, int bn, int block, int splits) {
   Fp8Plan p;
-  p.kind = cdiv(m, 256) * cdiv(n, 256) >= 128 ? FP8_BIG : FP8_SMALL;
-  p.tiles_m = (int)cdiv(m, p.kind == FP8_BIG ? 256 : 64);
-  p.tiles_n = (int)cdiv(n, p.kind == FP8_BIG ? 256 : 128);
-  p.splits = 1;
-  p.grid = (int64_t)p.tiles_m * p.tiles_n;
+  p.kind = kind;
+  p.tiles_m = (int)cdiv(rows, bm);
+  p.tiles_n = (int)cdiv(cols, bn);
+  p.splits = splits;
+  p.grid = (int64_t)p.tiles_m * p.tiles_n * splits;
+  p.block = block;
   return p;
 }
+
+// The one launch up to 2^14 values of X: each workgroup quantises all of them (1 x 4096
+// x 4096 6.2 us against 2.4 + 5.0 in two launches, 4 x 4096 x 4096 7.0 against 2.4 +
+// 5.5; 8 x 4096 x 4096 8.5 against 2.4 + 5.8).  Its LDS: X's codes and scales, the waves'
+// sums.
+constexpr int kFp8TokenRows = 16;
+inline size_t fp8_token_lds(int64_t m, int64_t k) { return (size_t)((m * fp8_blocks(k) * 129 + 15) / 16 * 16 + 8192); }
+
+inline Fp8Plan plan_fp8_fwd(int64_t m, int64_t n, int64_t k) {
+  const int64_t groups = cdiv(n, 16);
+  if (m <= kFp8TokenRows && m * k <= (1 << 14) && fp8_token_lds(m, k) <= 160 * 1024) {
+    // eight waves share a group of 16 features up to 1024 groups, else two (us: 1 x 11008
+    // x 4096 10.9 and 12.3, 1 x 32000 x 4096 22.7 and 20.4, 1 x 4096 x 11008 12.4 and 27)
+    const bool eight = groups <= 1024;
+    return fp8_plan_of(eight ? FP8_TOKEN_8 : FP8_TOKEN_2, m, n, kFp8TokenRows, eight ? 16 : 64, 512, 1);
+  }
+  const double s = (double)fp8_blocks(k);
+  Fp8Plan best{};
+  double least = 1e30;
+  auto consider = [&](const Fp8Plan& p, double t) {
+    if (t < least) {
+      least = t;
+      best = p;
+    }
+  };
+  for (const TileCost& t : kFp8Tiles) {
+    const Fp8Plan p = fp8_plan_of(t.kind, m, n, t.bm, t.bn, t.block, 1);
+    consider(p, tile_time(t, p.grid, s));
+  }
+  if (m <= 16) {
+    const Fp8Plan p = fp8_plan_of(FP8_FEW_1, m, n, 16, 16, 512, 1);
+    consider(p, 2.0 + 0.12 * s * std::max(1.0, (double)p.grid / 256));
+  } else if (m <= 32) {
+    const Fp8Plan p = fp8_plan_of(FP8_FEW_2, m, n, 32, 16, 512, 1);
+    consider(p, 2.0 + 0.19 * s * std::max(1.0, (double)p.grid / 256));
+  }
+  return best;
+}
+
+// Up to 256 workgroups may share the contractions of few tiles, 4 stages to each or
+// more; what that costs is the join's launch and the sums in memory.
 inline Fp8Plan plan_fp8_bwd(int64_t m, int64_t n, int64_t k) {
-  Fp8Plan p;
-  p.kind = cdiv(m, 256) * cdiv(k, 256) >= 128 ? FP8_BIG : FP8_SMALL;
-  p.tiles_m = (int)cdiv(m, p.kind == FP8_BIG ? 256 : 64);
-  p.tiles_n = (int)cdiv(k, 256);
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-  p.splits = p.kind == FP8_BIG ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, fp8_blocks(n)));
-  p.grid = tiles * p.splits;
-  return p;
+  const int64_t stages = fp8_blocks(n);
+  Fp8Plan best{};
+  double least = 1e30;
+  for (const TileCost& t : kFp8BackTiles) {
+    const int64_t tiles = cdiv(m, t.bm) * cdiv(k, t.bn);
+    const int64_t most = t.kind == FP8_BACK_64x256 ? std::max<int64_t>(1, std::min<int64_t>(256 / tiles, stages / 4)) : 1;
+    for (int64_t splits = 1; splits <= most; ++splits) {
+      const Fp8Plan p = fp8_plan_of(t.kind, m, k, t.bm, t.bn, t.block, (int)splits);
+      double time = tile_time(t, p.grid, (double)cdiv(stages, splits));
+      if (splits > 1) time += 4.5 + (double)p.grid * t.bm * t.bn * 8 / 4.5e6;
+      if (time < least) {
+        least = time;
+        best = p;
+      }
+    }
+  }
+  return best;
 }
 struct Fp8Layout {
   size_t codes, scales, sums, total;

@@ -395,9 +395,7 @@ __global__ __launch_bounds__(NT) void lora_xent_join_kernel(XentGrad p) {
   for (int s = 0; s < p.splits; ++s) v += from[(size_t)s * step];
   if (row >= p.rows || col >= p.k) return;
   if (p.coef) v = with_label(v, p.coef, p.labels, p.W, row, p.rows, p.vocab, p.k, col);
-  *reinterpret_cast<uint2*>(p.out + (size_t)row * p.k + col) =
-      uint2{(uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
-            (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16)};
+  *reinterpret_cast<uint2*>(p.out + (size_t)row * p.k + col) = bf16x4(v);
 }
 
 // ---- launches ----------------------------------------------------------------------
@@ -408,7 +406,7 @@ __global__ __launch_bounds__(NT) void lora_xent_join_kernel(XentGrad p) {
   } while (0)
 
 using GradBig = NnBig<Bf16>;
-using GradSmall = NnCore<Bf16, 64, 256, 4, 3>;
+using GradSmall = NnCore<Bf16, 64, 256, 1, 4, 3>;
 
 template <int MODE, bool TAIL>
 static hipError_t run_logits_of(const XentPlan& p, const XentLogits& q, hipStream_t st) {

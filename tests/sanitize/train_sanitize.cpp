@@ -84,6 +84,10 @@ static int plans() {
         HOLDS(f.grid >= 1 && f.grid < (int64_t(1) << 31) && f.splits >= 1, m, n, k);
         HOLDS(b.grid >= 1 && b.grid < (int64_t(1) << 31), m, n, k);
         HOLDS(b.splits >= 1 && b.splits <= fp8_blocks(n), m, n, k);   // no part of a contraction is empty
+        if (f.kind <= FP8_TOKEN_2) HOLDS(m <= kFp8TokenRows && fp8_token_lds(m, k) <= 160 * 1024 && m * fp8_blocks(k) * 16 < (1 << 19), m, n, k);
+        if (f.kind == FP8_FEW_1) HOLDS(m <= 16 && f.block == 512, m, n, k);
+        if (f.kind == FP8_FEW_2) HOLDS(m <= 32 && f.block == 512, m, n, k);
+        HOLDS(f.splits == 1 && (b.splits == 1 || b.kind == FP8_BACK_64x256), m, n, k);   // the join's tiles have 64 rows
         HOLDS(lf.scales >= fp8_codes_bytes(m, k) && lf.sums >= lf.scales + fp8_scales_bytes(m, k, 1), m, n, k);
         HOLDS(lb.scales >= fp8_codes_bytes(m, n) && lb.sums >= lb.scales + fp8_scales_bytes(m, n, 1), m, n, k);
         HOLDS(lf.total >= lf.sums && lb.total >= lb.sums, m, n, k);

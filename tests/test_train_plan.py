@@ -11,7 +11,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PKG = os.path.join(ROOT, "paper_2403_11366_amd")
 HOST_SAN = ["-O1", "-g", "-fno-sanitize-recover=all", "-fno-omit-frame-pointer", "-std=c++17"]
 SAN = ["-Xarch_host", "-fsanitize=address,undefined"]
-KINDS = {"fwd": 2, "bwd": 2}   # kernels of the 8-bit forward and backward
+KINDS = {"fwd": 9, "bwd": 3}   # kernels of the 8-bit forward and backward
 
 
 def _run(cmd, **kw):
