@@ -219,7 +219,11 @@ struct NtCore {
     const char *b0 = smem + wm * TM * 128 + f0, *b1 = smem + wm * TM * 128 + f1;
     const char* s0 = smem + SOFF + wave * 256 + c16 * 4;
     auto read = [&](int kb, auto place, auto set) LORA_INLINE {
-      constexpr int S = decltype(set)::value, O = decltype(place)::value * STAGE;
+      constexpr int S = decltype(set)::value;
+      int O = decltype(place)::value * STAGE;
+      // Addresses beyond the reads' own offsets are formed here where a wave's sums need the
+      // registers that keeping them for every place takes.
+      if (SMEM > 65536 && FA * FB >= 16) asm volatile("" : "+s"(O));
       if constexpr (E::SCALED) {
         sa[S] = bs.at(kb, 0);
 #pragma unroll

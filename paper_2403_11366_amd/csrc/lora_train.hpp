@@ -203,9 +203,18 @@ struct XentArgs {
   int64_t rows, vocab, k;
 };
 
-// Few rows take tiles of 64 rows (128 columns of logits, 256 of gradients), others
-// 256 x 256.
-//
+// The logits' tiles and those of dX, by estimated time (TileCost above; a stage of 64
+// bf16 columns moves and multiplies as much as one of 128 8-bit ones).
+enum XentTileKind { XENT_64x128, XENT_128x128, XENT_256x128, XENT_256x256 };
+enum XentGradKind { XENT_GRAD_64x256, XENT_GRAD_128x256, XENT_GRAD_256x256 };
+constexpr TileCost kXentTiles[4] = {{XENT_64x128, 64, 128, 256, 3.0, 0.45, 0.62},
+                                    {XENT_128x128, 128, 128, 512, 5.0, 0.50, 0.65},
+                                    {XENT_256x128, 256, 128, 512, 7.0, 0.78, 1.02},
+                                    {XENT_256x256, 256, 256, 512, 11.0, 1.03, 1.35}};
+constexpr TileCost kXentGradTiles[3] = {{XENT_GRAD_64x256, 64, 256, 256, 2.5, 0.71, 0.80},
+                                        {XENT_GRAD_128x256, 128, 256, 512, 4.5, 0.80, 0.93},
+                                        {XENT_GRAD_256x256, 256, 256, 512, 6.0, 1.03, 1.45}};
+
 // The vocabulary is walked in pieces: the exponentials (or gradients) of a piece's
 // logits in bf16 are the operand of the next product.  A piece's buffer is at most
 // 64 MiB (and a tile's width at least), so that it is still in the last-level cache
@@ -213,35 +222,68 @@ struct XentArgs {
 // workgroups.
 constexpr int64_t kPieceElems = int64_t(1) << 25;
 struct XentPlan {
-  bool big;
-  int tile_m, tile_n;          // of the logits' tiles
-  int tiles_m;
+  int kind, tile_m, tile_n;    // of the logits' tiles
+  int grad_kind, grad_m;       // of dX's
+  int tiles_m, grad_tiles_m;
   int vtiles, piece_tiles, pieces;   // tiles of the vocabulary, of a piece
   int64_t rows_pad, piece;     // padded rows, columns of a piece (its row pitch)
   int tiles_k, splits;         // column tiles of dX, parts of a piece that workgroups share
   int64_t stages;              // 64-column stages of a piece
 };
-inline XentPlan plan_xent(int64_t rows, int64_t vocab, int64_t k) {
-  XentPlan p;
-  p.big = rows > 128;
-  p.tile_m = p.big ? 256 : 64;
-  p.tile_n = p.big ? 256 : 128;
-  p.tiles_m = (int)cdiv(rows, p.tile_m);
-  p.rows_pad = (int64_t)p.tiles_m * p.tile_m;
-  p.vtiles = (int)cdiv(vocab, p.tile_n);
-  int64_t most = std::max<int64_t>(1, kPieceElems / p.rows_pad / p.tile_n);
-  if (most >= p.vtiles) most = p.vtiles;
-  else {
+inline XentPlan xent_plan_of(const TileCost& t, int64_t rows, int64_t vocab) {
+  XentPlan p{};
+  p.kind = t.kind;
+  p.tile_m = t.bm;
+  p.tile_n = t.bn;
+  p.tiles_m = (int)cdiv(rows, t.bm);
+  p.vtiles = (int)cdiv(vocab, t.bn);
+  int64_t most = std::max<int64_t>(1, kPieceElems / (cdiv(rows, 256) * 256) / t.bn);
+  if (most >= p.vtiles) {
+    most = p.vtiles;
+  } else {
     const int64_t rounds = (most * p.tiles_m + p.tiles_m - 1) / 256;
     if (rounds > 0) most = std::min(most, std::max<int64_t>(1, rounds * 256 / p.tiles_m));
   }
   p.piece_tiles = (int)most;
   p.pieces = (int)cdiv(p.vtiles, most);
-  p.piece = most * p.tile_n;
+  p.piece = most * t.bn;
   p.stages = p.piece / 64;
+  return p;
+}
+inline XentPlan plan_xent(int64_t rows, int64_t vocab, int64_t k) {
+  const double kstages = (double)cdiv(k, 64);
+  XentPlan p{};
+  double least = 1e30;
+  for (const TileCost& t : kXentTiles) {
+    const XentPlan q = xent_plan_of(t, rows, vocab);
+    const double time = (q.pieces - 1) * tile_time(t, (int64_t)q.tiles_m * q.piece_tiles, kstages) +
+                        tile_time(t, (int64_t)q.tiles_m * (q.vtiles - (int64_t)(q.pieces - 1) * q.piece_tiles), kstages);
+    if (time < least) {
+      least = time;
+      p = q;
+    }
+  }
   p.tiles_k = (int)cdiv(k, 256);
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_k;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, p.stages / 8));
+  least = 1e30;
+  for (const TileCost& t : kXentGradTiles) {
+    const int64_t tm = cdiv(rows, t.bm), tiles = tm * p.tiles_k;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, p.stages / 8));
+    for (int64_t splits = 1; splits <= most; ++splits) {
+      // (W's columns come from memory at 5.5 TB/s, whoever reads them first)
+      double time = std::max(tile_time(t, tiles * splits, (double)cdiv(p.stages, splits)), (double)(p.piece * k) * 2 / 5.5e6) +
+                    (double)(tiles * splits) * t.bm * 256 * 8 * (p.pieces > 1) / 4.5e6;
+      if (splits > 1) time += (4.5 + (double)(tiles * splits) * t.bm * 256 * 8 / 4.5e6) / p.pieces;
+      if (time < least) {
+        least = time;
+        p.grad_kind = t.kind;
+        p.grad_m = t.bm;
+        p.grad_tiles_m = (int)tm;
+        p.splits = (int)splits;
+      }
+    }
+  }
+  const int64_t pad = std::max(p.tile_m, p.grad_m);
+  p.rows_pad = cdiv(rows, pad) * pad;
   return p;
 }
 // Regions of the workspace.
@@ -268,7 +310,7 @@ inline XentLayout xent_layout(int64_t rows, int64_t vocab, int64_t k, bool dx, b
   L.piece = L.parts + region((size_t)p.vtiles * p.rows_pad * 8);
   L.turned = L.piece + (dx || dw ? region((size_t)(p.rows_pad * p.piece) * 2) : 0);
   L.sums = L.turned + (dw ? region((size_t)(p.rows_pad * p.piece) * 2) : 0);
-  L.saved = L.sums + (dx ? region((size_t)p.splits * p.tiles_m * p.tiles_k * p.tile_m * 256 * 4) : 0);
+  L.saved = L.sums + (dx ? region((size_t)p.splits * p.grad_tiles_m * p.tiles_k * p.grad_m * 256 * 4) : 0);
   L.total = L.saved + (dw ? region((size_t)rows * 8) : 0);
   return L;
 }

@@ -405,40 +405,58 @@ __global__ __launch_bounds__(NT) void lora_xent_join_kernel(XentGrad p) {
     if (e_ != hipSuccess) return e_; \
   } while (0)
 
-using GradBig = NnBig<Bf16>;
-using GradSmall = NnCore<Bf16, 64, 256, 1, 4, 3>;
-
 template <int MODE, bool TAIL>
 static hipError_t run_logits_of(const XentPlan& p, const XentLogits& q, hipStream_t st) {
   const int tiles = q.tiles_m * q.tiles_n;
   const dim3 grid((unsigned)(MODE == XENT_AGAIN ? std::min(tiles, 256) : tiles));
-  if (p.big)
-    hipLaunchKernelGGL((lora_xent_logits_kernel<NtBig<Bf16, TAIL>, 256, 256, 512, MODE>), grid, dim3(512), 0, st, q);
-  else
-    hipLaunchKernelGGL((lora_xent_logits_kernel<NtCore<Bf16, 64, 128, 1, 4, 6, TAIL>, 64, 128, 256, MODE>), grid,
-                       dim3(256), 0, st, q);
+  switch (p.kind) {
+    case XENT_64x128:
+      hipLaunchKernelGGL((lora_xent_logits_kernel<NtCore<Bf16, 64, 128, 1, 4, 6, TAIL>, 64, 128, 256, MODE>), grid,
+                         dim3(256), 0, st, q);
+      break;
+    case XENT_128x128:
+      hipLaunchKernelGGL((lora_xent_logits_kernel<NtCore<Bf16, 128, 128, 2, 4, 4, TAIL>, 128, 128, 512, MODE>), grid,
+                         dim3(512), 0, st, q);
+      break;
+    case XENT_256x128:
+      hipLaunchKernelGGL((lora_xent_logits_kernel<NtCore<Bf16, 256, 128, 4, 2, 3, TAIL>, 256, 128, 512, MODE>), grid,
+                         dim3(512), 0, st, q);
+      break;
+    default:
+      hipLaunchKernelGGL((lora_xent_logits_kernel<NtBig<Bf16, TAIL>, 256, 256, 512, MODE>), grid, dim3(512), 0, st, q);
+  }
   return hipGetLastError();
 }
 template <int MODE>
 static hipError_t run_logits(const XentPlan& p, const XentLogits& q, hipStream_t st) {
   return q.k % 64 ? run_logits_of<MODE, true>(p, q, st) : run_logits_of<MODE, false>(p, q, st);
 }
+using Grad64 = NnCore<Bf16, 64, 256, 1, 4, 3>;
+using Grad128 = NnCore<Bf16, 128, 256, 2, 4, 3>;
+using Grad256 = NnBig<Bf16>;
 template <int END>
-static hipError_t run_grad_of(bool big, const XentGrad& q, hipStream_t st) {
+static hipError_t run_grad_of(int kind, const XentGrad& q, hipStream_t st) {
   const dim3 grid((unsigned)(q.tiles_m * q.tiles_n * q.splits));
-  if (big) hipLaunchKernelGGL((lora_xent_grad_kernel<GradBig, 256, 512, END>), grid, dim3(512), 0, st, q);
-  else hipLaunchKernelGGL((lora_xent_grad_kernel<GradSmall, 64, 256, END>), grid, dim3(256), 0, st, q);
+  switch (kind) {
+    case XENT_GRAD_64x256: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad64, 64, 256, END>), grid, dim3(256), 0, st, q); break;
+    case XENT_GRAD_128x256: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad128, 128, 512, END>), grid, dim3(512), 0, st, q); break;
+    default: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad256, 256, 512, END>), grid, dim3(512), 0, st, q);
+  }
   return hipGetLastError();
 }
-static hipError_t run_grad(bool big, const XentGrad& q, hipStream_t st) {
-  if (!q.last) return run_grad_of<XENT_CARRY>(big, q, st);
-  return q.coef ? run_grad_of<XENT_LABEL>(big, q, st) : run_grad_of<XENT_STORE>(big, q, st);
+static hipError_t run_grad(int kind, const XentGrad& q, hipStream_t st) {
+  if (!q.last) return run_grad_of<XENT_CARRY>(kind, q, st);
+  return q.coef ? run_grad_of<XENT_LABEL>(kind, q, st) : run_grad_of<XENT_STORE>(kind, q, st);
 }
-static hipError_t run_join(bool big, const XentGrad& q, hipStream_t st) {
-  const int tiles = q.tiles_m * q.tiles_n;
-  if (big) hipLaunchKernelGGL((lora_xent_join_kernel<GradBig, 256, 512>), dim3((unsigned)(tiles * 32)), dim3(512), 0, st, q);
-  else hipLaunchKernelGGL((lora_xent_join_kernel<GradSmall, 64, 256>), dim3((unsigned)(tiles * 16)), dim3(256), 0, st, q);
+template <class Core, int BM, int NT>
+static hipError_t run_join_of(const XentGrad& q, hipStream_t st) {
+  constexpr int F = std::extent_v<typename Core::Acc, 0> * std::extent_v<typename Core::Acc, 1>;
+  hipLaunchKernelGGL((lora_xent_join_kernel<Core, BM, NT>), dim3((unsigned)(q.tiles_m * q.tiles_n * F)), dim3(NT), 0, st, q);
   return hipGetLastError();
+}
+static hipError_t run_join(int kind, const XentGrad& q, hipStream_t st) {
+  if (kind == XENT_GRAD_64x256) return run_join_of<Grad64, 64, 256>(q, st);
+  return kind == XENT_GRAD_128x256 ? run_join_of<Grad128, 128, 512>(q, st) : run_join_of<Grad256, 256, 512>(q, st);
 }
 
 struct XentCall {
@@ -479,7 +497,7 @@ struct XentCall {
     g.b_rows = std::min(p.piece, a.vocab - v0);
     g.m = (int)p.rows_pad; g.rows = (int)a.rows; g.vocab = (int)a.vocab; g.k = (int)a.k;
     g.stages = (int)cdiv(g.b_rows, 64);
-    g.tiles_m = p.tiles_m; g.tiles_n = p.tiles_k; g.splits = p.splits;   // (some have nothing but their scaling to do in a short last piece)
+    g.tiles_m = p.grad_tiles_m; g.tiles_n = p.tiles_k; g.splits = p.splits;   // (some have nothing but their scaling to do in a short last piece)
     return g;
   }
   hipError_t rows(float* saved, float* coef) const {
@@ -504,7 +522,7 @@ struct XentCall {
     for (int i = 0; i < p.pieces; ++i) {
       at_piece(q, i);
       LORA_TRY(run_logits<XENT_GRAD>(p, q, st));
-      if (a.dX) LORA_TRY(run_grad(p.big, dx(i), st));
+      if (a.dX) LORA_TRY(run_grad(p.grad_kind, dx(i), st));
       if (a.dW) {
         const int64_t v0 = i * p.piece, cols = std::min(p.piece, a.vocab - v0);
         XentGrad g{};
@@ -512,12 +530,12 @@ struct XentCall {
         g.a_cols = p.rows_pad; g.b_rows = a.rows;
         g.first = g.last = true;
         g.m = g.rows = (int)cols; g.k = (int)a.k;
-        g.stages = (int)(p.rows_pad / 64);
+        g.stages = (int)cdiv(a.rows, 64);   // (columns of `turned` that tiles have written)
         g.tiles_m = (int)cdiv(cols, 256); g.tiles_n = p.tiles_k; g.splits = 1;
-        LORA_TRY(run_grad(true, g, st));
+        LORA_TRY(run_grad(XENT_GRAD_256x256, g, st));
       }
     }
-    return a.dX && p.splits > 1 ? run_join(p.big, dx(0), st) : hipSuccess;
+    return a.dX && p.splits > 1 ? run_join(p.grad_kind, dx(0), st) : hipSuccess;
   }
   // Loss and dX, the logits formed once.
   hipError_t one_pass() const {
@@ -541,12 +559,12 @@ struct XentCall {
       if (g.last) g.coef = coef;
       g.ref_old = q.ref;
       g.ref = q.ref_next;
-      LORA_TRY(run_grad(p.big, g, st));
+      LORA_TRY(run_grad(p.grad_kind, g, st));
     }
     if (p.splits == 1) return hipSuccess;
     XentGrad g = dx(0);
     g.coef = coef;
-    return run_join(p.big, g, st);
+    return run_join(p.grad_kind, g, st);
   }
 };
 

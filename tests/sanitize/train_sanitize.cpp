@@ -5,7 +5,7 @@
 // before any HIP call.  Device pointers are fake addresses that validation never reads.
 //
 // With arguments "fwd" or "bwd" and m n k m n k ... it prints the kernel kind of each
-// 8-bit call.
+// 8-bit call, with "xent" and rows vocab k ... those of the loss.
 #include <stdint.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -101,11 +101,12 @@ static int plans() {
       for (int64_t k : {8, 72, 512, 4096, 5120, 8200, 1 << 16}) {
         if (lora_linear_xent_workspace_size(rows, vocab, k, 0, 0) == 0) continue;
         const XentPlan p = plan_xent(rows, vocab, k);
-        HOLDS(p.rows_pad >= rows && p.rows_pad % 64 == 0 && p.rows_pad == (int64_t)p.tiles_m * p.tile_m, rows, vocab, k);
+        HOLDS((int64_t)p.tiles_m * p.tile_m >= rows && p.rows_pad >= (int64_t)p.tiles_m * p.tile_m && p.rows_pad % p.tile_m == 0, rows, vocab, k);
+        HOLDS(p.rows_pad >= (int64_t)p.grad_tiles_m * p.grad_m && (int64_t)p.grad_tiles_m * p.grad_m >= rows, rows, vocab, k);
         HOLDS((int64_t)p.vtiles * p.tile_n >= vocab && (int64_t)(p.vtiles - 1) * p.tile_n < vocab, rows, vocab, k);
         HOLDS((int64_t)p.pieces * p.piece_tiles >= p.vtiles && (int64_t)(p.pieces - 1) * p.piece_tiles < p.vtiles, rows, vocab, k);
         HOLDS(p.piece == (int64_t)p.piece_tiles * p.tile_n && p.piece % 64 == 0 && p.stages * 64 == p.piece, rows, vocab, k);
-        HOLDS((int64_t)p.tiles_m * p.vtiles < (int64_t(1) << 31) && (int64_t)p.tiles_m * p.tiles_k * p.splits < (int64_t(1) << 28), rows, vocab, k);
+        HOLDS((int64_t)p.tiles_m * p.vtiles < (int64_t(1) << 31) && (int64_t)p.grad_tiles_m * p.tiles_k * p.splits < (int64_t(1) << 28), rows, vocab, k);
         HOLDS(p.splits >= 1, rows, vocab, k);
         // what the tiles' 32-bit offsets reach: 256 rows of each operand
         HOLDS(p.piece * 2 * p.tile_m < (int64_t(1) << 31) && p.rows_pad * 2 * 256 < (int64_t(1) << 31) && k * 2 * 256 < (int64_t(1) << 31), rows, vocab, k);
@@ -116,7 +117,7 @@ static int plans() {
           HOLDS(L.piece - L.parts >= (size_t)(p.vtiles * p.rows_pad * 8), rows, vocab, k);
           if (d) HOLDS(L.turned - L.piece >= (size_t)(p.rows_pad * p.piece * 2), rows, vocab, k);
           if (d & 2) HOLDS(L.sums - L.turned >= (size_t)(p.rows_pad * p.piece * 2) && L.total - L.saved >= (size_t)(rows * 8), rows, vocab, k);
-          if (d & 1) HOLDS(L.saved - L.sums >= (size_t)p.splits * p.rows_pad * p.tiles_k * 256 * 4, rows, vocab, k);
+          if (d & 1) HOLDS(L.saved - L.sums >= (size_t)p.splits * p.grad_tiles_m * p.grad_m * p.tiles_k * 256 * 4, rows, vocab, k);
           if (d != 2) HOLDS(L.total >= last, rows, vocab, k);   // a call with fewer outputs needs no more
           last = d == 2 ? last : L.total;
           ++checked;
@@ -129,6 +130,11 @@ int main(int argc, char** argv) {
   if (argc > 1) {
     for (int i = 2; i + 2 < argc; i += 3) {
       const int64_t m = atoll(argv[i]), n = atoll(argv[i + 1]), k = atoll(argv[i + 2]);
+      if (strcmp(argv[1], "xent") == 0) {   // rows, vocab, k: its kernels, and whether there are parts to join and pieces
+        const lora::XentPlan p = lora::plan_xent(m, n, k);
+        printf("logits%d grad%d join%d pieces%d\n", p.kind, p.grad_kind, p.splits > 1 ? p.grad_kind : -1, p.pieces > 1);
+        continue;
+      }
       printf("%d\n", (int)(strcmp(argv[1], "fwd") == 0 ? lora::plan_fp8_fwd(m, n, k) : lora::plan_fp8_bwd(m, n, k)).kind);
     }
     return 0;

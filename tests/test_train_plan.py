@@ -49,3 +49,12 @@ def test_gpu_sizes_reach_every_kernel_of_the_8_bit_layer(driver, way):
     sizes = [str(x) for m, n, k in gpu.LINEAR for x in ((m, n, k) if way == "fwd" else (m, k, n))]
     text = _run([driver, way] + sizes, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
     assert set(text.split()) == {str(i) for i in range(KINDS[way])}
+
+
+def test_gpu_sizes_reach_every_kernel_of_the_loss(driver):
+    import test_gpu_xent as gpu
+    sizes = [str(x) for shape in gpu.SIZES + [(4100, 20011, 72)] for x in shape]
+    text = _run([driver, "xent"] + sizes, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+    want = {f"logits{i}" for i in range(4)} | {f"grad{i}" for i in range(3)} | {f"join{i}" for i in range(3)} | \
+        {"join-1", "pieces0", "pieces1"}
+    assert set(text.split()) == want
