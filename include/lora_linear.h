@@ -561,7 +561,7 @@ lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtyp
  *   X         [rows, k] bf16, read only
  *   W         [vocab, k] bf16, read only
  *   labels    [rows].  A label outside [0, vocab) is none: the row's loss is 0 and it
- *             has no part in the gradients (for dW its X has to be finite)
+ *             has no part in the gradients, whatever its X holds
  *   loss      [rows] fp32, written
  *   saved     [rows, 2] fp32: written by the forward for the backward (there may be
  *             NULL)

@@ -143,13 +143,14 @@ def _ptr(t) -> int:
 # torch's types and the current stream's handle as a call (a
 # torch.cuda.Stream object per call costs a microsecond), looked up on the
 # first call that needs them: the host-only functions do without torch.
-_BF16 = _F32 = _I32 = _U8 = _current_stream = None
+_BF16 = _F32 = _I32 = _U8 = _current_stream = _current_device = None
 
 
 def _bind_torch() -> None:
-    global _BF16, _F32, _I32, _U8, _current_stream
+    global _BF16, _F32, _I32, _U8, _current_stream, _current_device
     import torch
     raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    _current_device = device if device is not None else torch.cuda.current_device
     if raw is not None and device is not None:
         _current_stream = lambda: raw(device())
     else:
@@ -600,6 +601,14 @@ def lora_distill_step(logits, teacher_ids, teacher_logits, labels, dloss, loss, 
         raise LoraError(st, "lora_distill_step")
 
 
+def _same_device(*tensors) -> None:
+    """The tensors (None: left out) lie on the current device, where the call launches."""
+    device = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{device}")
+
+
 def lora_fp8_codes_size(rows: int, k: int) -> int:
     return int(load_library().lora_fp8_codes_size(rows, k))
 
@@ -633,6 +642,7 @@ def lora_fp8_quantize(X, codes, scales, block_rows: int = 128, stream=None) -> N
     if not _fits(X, _BF16, (rows, k)):
         _check(X, "X", _BF16, (rows, k))
     _check_fp8(codes, scales, rows, k, block_rows)
+    _same_device(X, codes, scales)
     st = load_library().lora_fp8_quantize(_ptr(X), _ptr(codes), _ptr(scales), rows, k, block_rows, _stream_handle(stream))
     if st != 0:
         raise LoraError(st, "lora_fp8_quantize")
@@ -646,6 +656,7 @@ def lora_fp8_dequantize(codes, scales, X, block_rows: int = 128, stream=None) ->
     if not _fits(X, _BF16, (rows, k)):
         _check(X, "X", _BF16, (rows, k))
     _check_fp8(codes, scales, rows, k, block_rows)
+    _same_device(codes, scales, X)
     st = load_library().lora_fp8_dequantize(_ptr(codes), _ptr(scales), _ptr(X), rows, k, block_rows,
                                             _stream_handle(stream))
     if st != 0:
@@ -675,6 +686,7 @@ def lora_linear_fp8_fwd(X, W_codes, W_scales, Y, workspace, stream=None) -> None
         _check(Y, "Y", _BF16, (m, n))
     _check_fp8(W_codes, W_scales, n, k, 128, "W_")
     ws_bytes = _workspace_bytes(workspace)
+    _same_device(X, W_codes, W_scales, Y, workspace)
     st = load_library().lora_linear_fp8_fwd(_ptr(X), _ptr(W_codes), _ptr(W_scales), _ptr(Y), _ptr(workspace), ws_bytes,
                                             m, n, k, _stream_handle(stream))
     if st != 0:
@@ -695,6 +707,7 @@ def lora_linear_fp8_bwd(dY, W_codes, W_scales, dX, workspace, stream=None) -> No
         _check(dX, "dX", _BF16, (m, k))
     _check_fp8(W_codes, W_scales, n, k, 128, "W_")
     ws_bytes = _workspace_bytes(workspace)
+    _same_device(dY, W_codes, W_scales, dX, workspace)
     st = load_library().lora_linear_fp8_bwd(_ptr(dY), _ptr(W_codes), _ptr(W_scales), _ptr(dX), _ptr(workspace), ws_bytes,
                                             m, n, k, _stream_handle(stream))
     if st != 0:
@@ -716,6 +729,7 @@ def lora_dropout(X, Y, seed: int, offset: int, p: float, residual=None, stream=N
     for t, name in ((X, "X"), (Y, "Y"), (residual, "residual")):
         if t is not None and not _fits(t, X.dtype, X.shape):
             _check(t, name, X.dtype, X.shape)
+    _same_device(X, Y, residual)
     st = load_library().lora_dropout(_ptr(X), _ptr(residual), _ptr(Y), 1 if X.dtype is _F32 else 0, X.numel(),
                                      int(seed) & 0xFFFFFFFFFFFFFFFF, int(offset) & 0xFFFFFFFFFFFFFFFF, float(p),
                                      _stream_handle(stream))
@@ -757,6 +771,7 @@ def lora_linear_xent_fwd(X, W, labels, loss, saved, workspace, stream=None) -> N
     if saved is not None:
         _check_rows((saved, "saved", _F32, (rows, 2)))
     ws_bytes = _workspace_bytes(workspace)
+    _same_device(X, W, labels, loss, saved, workspace)
     st = load_library().lora_linear_xent_fwd(_ptr(X), _ptr(W), _ptr(labels), _ptr(loss), _ptr(saved), _ptr(workspace),
                                              ws_bytes, rows, vocab, k, _stream_handle(stream))
     if st != 0:
@@ -772,6 +787,7 @@ def lora_linear_xent_bwd(X, W, labels, saved, dloss, dX, dW, workspace, stream=N
     _check_rows((saved, "saved", _F32, (rows, 2)))
     _check_xent_grads(dX, dW, dloss, rows, vocab, k)
     ws_bytes = _workspace_bytes(workspace)
+    _same_device(X, W, labels, saved, dloss, dX, dW, workspace)
     st = load_library().lora_linear_xent_bwd(_ptr(X), _ptr(W), _ptr(labels), _ptr(saved), _ptr(dloss), _ptr(dX),
                                              _ptr(dW), _ptr(workspace), ws_bytes, rows, vocab, k, _stream_handle(stream))
     if st != 0:
@@ -785,6 +801,7 @@ def lora_linear_xent_step(X, W, labels, dloss, loss, dX, dW, workspace, stream=N
     _check_rows((loss, "loss", _F32, (rows,)))
     _check_xent_grads(dX, dW, dloss, rows, vocab, k)
     ws_bytes = _workspace_bytes(workspace)
+    _same_device(X, W, labels, dloss, loss, dX, dW, workspace)
     st = load_library().lora_linear_xent_step(_ptr(X), _ptr(W), _ptr(labels), _ptr(dloss), _ptr(loss), _ptr(dX), _ptr(dW),
                                               _ptr(workspace), ws_bytes, rows, vocab, k, _stream_handle(stream))
     if st != 0:

@@ -35,8 +35,8 @@ __global__ __launch_bounds__(256) void lora_dropout_kernel(const void* X, const 
       if constexpr (RES) r[i] = static_cast<const int4v*>(R)[W * t + i];
     }
   }
-  uint64_t c[4];
-  philox_block(seed, offset, (uint64_t)t, c);
+  uint64_t c[4] = {0ull, 0ull, 0ull, 0ull};
+  if (thr < 65536u) philox_block(seed, offset, (uint64_t)t, c);   // (p = 0 keeps every draw)
   auto value = [&](int e, float xv, float rv) LORA_INLINE {
     const float y = philox_draw(c, e) < thr ? xv * scale : 0.0f;
     return RES ? y + rv : y;

@@ -53,20 +53,32 @@ __device__ __forceinline__ int fp8_row_scale_at(int row, int block, int cells) {
   return (block * cells + (row >> 6)) * 64 + (row & 15) * 4 + ((row >> 4) & 3);
 }
 
-// Activations: 16 lanes a row's block, 8 columns each.
+// Activations: 16 lanes a row's block, 8 columns each; a thread takes rows 16 apart,
+// whose scales are a word.  A workgroup: four blocks of the rows of a quarter cell
+// (its rows 4 q .. 4 q + 3, and those 16, 32 and 48 after them).
 __global__ __launch_bounds__(256) void lora_fp8_quantize_rows_kernel(const u16* __restrict__ X,
                                                                      uint8_t* __restrict__ codes,
                                                                      uint8_t* __restrict__ scales, int rows, int k,
                                                                      int blocks, int cells) {
-  const int64_t e = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int row = (int)(e / blocks), b = (int)(e - (int64_t)row * blocks);
-  if (row >= cells * 64) return;
-  const int j = threadIdx.x & 15, col = b * 128 + 8 * j;
-  int4v x{0, 0, 0, 0};
-  if (row < rows && col < k) x = *reinterpret_cast<const int4v*>(X + (size_t)row * k + col);
-  const int s = fp8_scale(max16(top_of(x)));
-  if (row < rows) *reinterpret_cast<int2w*>(codes + ((size_t)row * blocks + b) * 128 + 8 * j) = fp8_codes(x, s);
-  if (j == 0) scales[fp8_row_scale_at(row, b, cells)] = (uint8_t)(row < rows ? s : 0);
+  const int groups = (blocks + 3) / 4, bg = (int)blockIdx.x % groups, rest = (int)blockIdx.x / groups;
+  const int cell = rest >> 2, tid = threadIdx.x, lane16 = tid & 15;
+  const int b = bg * 4 + ((tid >> 4) & 3), r16 = 4 * (rest & 3) + (tid >> 6), col = b * 128 + 8 * lane16;
+  if (b >= blocks) return;   // (16 lanes alike)
+  int4v x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = cell * 64 + r16 + 16 * i;
+    x[i] = row < rows && col < k ? *reinterpret_cast<const int4v*>(X + (size_t)row * k + col) : int4v{0, 0, 0, 0};
+  }
+  uint32_t word = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = cell * 64 + r16 + 16 * i, s = fp8_scale(max16(top_of(x[i])));
+    if (row >= rows) continue;
+    word |= (uint32_t)s << (8 * i);
+    *reinterpret_cast<int2w*>(codes + ((size_t)row * blocks + b) * 128 + 8 * lane16) = fp8_codes(x[i], s);
+  }
+  if (lane16 == 0) *reinterpret_cast<uint32_t*>(scales + fp8_row_scale_at(cell * 64 + r16, b, cells)) = word;
 }
 
 // A weight: a workgroup a block of 128 x 128.
@@ -353,8 +365,7 @@ __global__ __launch_bounds__(256) void lora_fp8_join_kernel(const float* __restr
 hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, hipStream_t st) {
   const int blocks = (int)fp8_blocks(a.k), cells = (int)fp8_cells(a.rows);
   if (a.block_rows == 1)
-    hipLaunchKernelGGL(lora_fp8_quantize_rows_kernel, dim3((unsigned)cdiv((int64_t)cells * 64 * blocks, 16)), dim3(256),
-                       0, st, a.X, a.codes, a.scales, (int)a.rows, (int)a.k, blocks, cells);
+    hipLaunchKernelGGL(lora_fp8_quantize_rows_kernel, dim3((unsigned)(cells * 4 * (int)cdiv(blocks, 4))), dim3(256), 0, st, a.X, a.codes, a.scales, (int)a.rows, (int)a.k, blocks, cells);
   else
     hipLaunchKernelGGL(lora_fp8_quantize_block_kernel, dim3((unsigned)(cdiv(a.rows, 128) * blocks)), dim3(256), 0, st,
                        a.X, a.codes, a.scales, (int)a.rows, (int)a.k, blocks);

@@ -305,6 +305,25 @@ struct Panel {
   }
 };
 
+// bf16 values of at most 1, not negative, times 2^-(shift / 128): below 2^-126 nearly
+// or quite 0.
+__device__ __forceinline__ int4v scaled_down(int4v v, uint32_t shift) {
+  typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+  const ushort2v by{(unsigned short)shift, (unsigned short)shift};
+#pragma unroll
+  for (int h = 0; h < 4; ++h)
+    v[h] = __builtin_bit_cast(int, __builtin_elementwise_sub_sat(__builtin_bit_cast(ushort2v, (int)v[h]), by));
+  return v;
+}
+// Powers of two that a core's A is multiplied by where it is read: a number per row and
+// 2^log stages.
+template <int ROWS>
+struct Shifts {
+  const u16* table;   // [stages from `first` on, >> log][ROWS] in LDS
+  int first, log;
+  __device__ __forceinline__ uint32_t at(int stage, int row) const { return table[((stage >> log) - first) * ROWS + row]; }
+};
+
 // C = A B, BM x BN (BN 128 or 256) by WM x WN waves, NS stages.
 template <class E, int BM, int BN, int WM, int WN, int NS>
 struct NnCore {
@@ -317,8 +336,9 @@ struct NnCore {
   static __device__ __forceinline__ int col(int wave, int a) { return wave % WN * TN + 16 * a; }
 
   // stages [s0, s1) of the contraction
+  template <bool SHIFT = false>
   static __device__ __forceinline__ void run(const NnTile& t, const Scales& sc, int m0, int s0, int s1, char* smem,
-                                             Acc& acc) {
+                                             Acc& acc, const Shifts<BM>& shifts = {}) {
     using P = Panel<E>;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int wm = wave / WN, wn = wave % WN, g = lane >> 4, c16 = lane & 15, l8 = lane >> 3;
@@ -373,6 +393,7 @@ struct NnCore {
     Frag fb[2][FB];              // of this stage and the next
     int2w w[2][FA][4];
     int sa[2] = {}, sw[2] = {};
+    uint32_t down[2][FB];
     static_assert(FA == 4, "the wait's operands");
     const uint32_t f0 = kc_offset(c16, g), f1 = f0 ^ 64;
     const char *b0 = smem + wm * TM * 128 + f0, *b1 = smem + wm * TM * 128 + f1;
@@ -385,6 +406,9 @@ struct NnCore {
 #pragma unroll
       for (int b = 0; b < FB; ++b)
         fb[S][b] = Frag{*reinterpret_cast<const int4v*>(b0 + O + 2048 * b), *reinterpret_cast<const int4v*>(b1 + O + 2048 * b)};
+      if constexpr (SHIFT)
+#pragma unroll
+        for (int b = 0; b < FB; ++b) down[S][b] = shifts.at(min(kb, s1 - 1), wm * TM + 16 * b + c16);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int a = 0; a < FA; ++a) {
@@ -408,6 +432,7 @@ struct NnCore {
       constexpr int S = decltype(set)::value;
       each_of<FB>([&](auto bc) LORA_INLINE {
         constexpr int B = decltype(bc)::value;
+        if constexpr (SHIFT) fb[S][B] = Frag{scaled_down(fb[S][B].lo, down[S][B]), scaled_down(fb[S][B].hi, down[S][B])};
 #pragma unroll
         for (int a = 0; a < FA; ++a) {
           Frag f;

@@ -229,7 +229,11 @@ struct XentPlan {
   int64_t rows_pad, piece;     // padded rows, columns of a piece (its row pitch)
   int tiles_k, splits;         // column tiles of dX, parts of a piece that workgroups share
   int64_t stages;              // 64-column stages of a piece
+  bool local;                  // the one-pass call takes a tile's powers against the tile's own largest
 };
+// Tiles of logits whose references a workgroup of dX holds in LDS: 64 rows' 256 in 32
+// KiB, 128 rows' 40 in 10 KiB beside its stages.
+constexpr int local_tiles(int grad_m) { return grad_m == 64 ? 256 : 40; }
 inline XentPlan xent_plan_of(const TileCost& t, int64_t rows, int64_t vocab) {
   XentPlan p{};
   p.kind = t.kind;
@@ -282,6 +286,8 @@ inline XentPlan plan_xent(int64_t rows, int64_t vocab, int64_t k) {
       }
     }
   }
+  p.local = p.pieces == 1 && p.grad_kind != XENT_GRAD_256x256 &&
+            cdiv(p.stages, p.splits) / (p.tile_n / 64) + 2 <= local_tiles(p.grad_m);
   const int64_t pad = std::max(p.tile_m, p.grad_m);
   p.rows_pad = cdiv(rows, pad) * pad;
   return p;
@@ -295,6 +301,7 @@ struct XentLayout {
   size_t parts;    // [tile][rows_pad] reference and sum of each tile's rows
   size_t piece;    // [rows_pad][piece] exponentials or gradients of a piece
   size_t turned;   // [piece][rows_pad] the latter turned, for dW
+  size_t known;    // [rows][k] X, zero in rows without a label, for dW
   size_t sums;     // [split][tile] fp32 sums of dX
   size_t saved;    // of the forward, in a call that runs both
   size_t total;
@@ -309,7 +316,8 @@ inline XentLayout xent_layout(int64_t rows, int64_t vocab, int64_t k, bool dx, b
   L.parts = L.best + region((size_t)p.rows_pad * 8);
   L.piece = L.parts + region((size_t)p.vtiles * p.rows_pad * 8);
   L.turned = L.piece + (dx || dw ? region((size_t)(p.rows_pad * p.piece) * 2) : 0);
-  L.sums = L.turned + (dw ? region((size_t)(p.rows_pad * p.piece) * 2) : 0);
+  L.known = L.turned + (dw ? region((size_t)(p.rows_pad * p.piece) * 2) : 0);
+  L.sums = L.known + (dw ? region((size_t)(rows * k) * 2) : 0);
   L.saved = L.sums + (dx ? region((size_t)p.splits * p.grad_tiles_m * p.tiles_k * p.grad_m * 256 * 4) : 0);
   L.total = L.saved + (dw ? region((size_t)rows * 8) : 0);
   return L;

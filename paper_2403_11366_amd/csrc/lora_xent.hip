@@ -16,7 +16,10 @@
 // fp32 hold 2^126): then the tiles of those rows are formed again against the
 // maximum, and what is carried is scaled.  So any logits come out right, and
 // ordinary ones at the price of two products and, for each piece, of a launch that
-// finds nothing to do (4 us).  A gradient of W needs the normaliser
+// finds nothing to do (4 us).  For few rows, whose piece is the whole vocabulary, that
+// launch and the references' are saved: a tile's powers are taken against its own
+// largest, rounded up to a power of two, and the second product, which knows the row's
+// by then, subtracts the difference from their exponents where it reads them.  A gradient of W needs the normaliser
 // in front of its sum over rows: with dW the forward runs first, and the logits are
 // formed again.
 //
@@ -38,7 +41,7 @@ struct Part {   // of a row's logits in a tile: reference, sum of powers against
   float m, s;
 };
 
-enum XentMode { XENT_STATS, XENT_PIECE, XENT_AGAIN, XENT_GRAD };
+enum XentMode { XENT_STATS, XENT_PIECE, XENT_AGAIN, XENT_LOCAL, XENT_GRAD };
 
 struct XentLogits {
   const u16 *X, *W;
@@ -50,6 +53,7 @@ struct XentLogits {
   uint32_t* best_next;
   const float* saved;    // XENT_GRAD: of the forward
   const float* dloss;
+  float* coef;           // XENT_GRAD of the first piece: [rows_pad][2], written (or none)
   Part* parts;           // [tile][rows_pad]
   u16 *piece, *turned;   // [rows_pad][piece], [piece][rows_pad]
   int rows, vocab, k, tiles_m, tiles_n, tile0;
@@ -77,7 +81,7 @@ struct XentTile {
   static constexpr int FA = std::extent_v<typename Core::Acc, 0>, FB = std::extent_v<typename Core::Acc, 1>;
   static constexpr int NW = NT / 64, TM = 16 * FB, WN = NW / (BM / TM);
   static constexpr int SMEM = Core::SMEM > BM * BN * 2 ? Core::SMEM : BM * BN * 2;
-  static constexpr bool EXPS = MODE == XENT_PIECE || MODE == XENT_AGAIN;   // powers against ref
+  static constexpr bool EXPS = MODE == XENT_PIECE || MODE == XENT_AGAIN || MODE == XENT_LOCAL;   // powers against ref
   struct Lds {
     char stages[SMEM];
     Part joined[WN][BM];
@@ -97,28 +101,33 @@ struct XentTile {
     const int lane = lane_fresh(), tid = threadIdx.x, wave = uniform(tid >> 6), g = lane >> 4, c16 = lane & 15;
     const int r0 = Core::row0(wave), wn = wave % WN, c0 = n0 + Core::col(wave, 0);
     // Few waves see a label among their 16 FA columns, and few tiles the vocabulary's end.
+    auto largest = [&](auto bc, auto plain) LORA_INLINE {   // of a lane's logits of a row but the label's
+      constexpr int b = decltype(bc)::value;
+      const int i = r0 + 16 * b + c16, y = lds.label[i];
+      float top = -INFINITY;
+#pragma unroll
+      for (int a = 0; a < FA; ++a)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float z = acc[a][b][q];
+          if constexpr (decltype(plain)::value) {
+            top = fmaxf(top, z);
+          } else {
+            const int col = n0 + Core::col(wave, a) + 4 * g + q;
+            if (col == y && MODE != XENT_AGAIN) p.zy[m0 + i] = z;
+            if (col < p.vocab && col != y) top = fmaxf(top, z);
+          }
+        }
+      return top;
+    };
     auto rows_of = [&](auto bc, auto plain) LORA_INLINE {
       constexpr int b = decltype(bc)::value;
       constexpr bool PLAIN = decltype(plain)::value;
       const int i = r0 + 16 * b + c16, y = lds.label[i];
       const float r = MODE == XENT_STATS ? 0.0f : lds.ref[i];
       if constexpr (MODE != XENT_GRAD) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int a = 0; a < FA; ++a)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float z = acc[a][b][q];
-            if constexpr (PLAIN) {
-              top = fmaxf(top, z);
-            } else {
-              const int col = n0 + Core::col(wave, a) + 4 * g + q;
-              if (col == y && MODE != XENT_AGAIN) p.zy[m0 + i] = z;
-              if (col < p.vocab && col != y) top = fmaxf(top, z);
-            }
-          }
-        float base = r;
-        if constexpr (MODE != XENT_AGAIN) {
+        float top = MODE == XENT_LOCAL ? -INFINITY : largest(bc, plain), base = r;
+        if constexpr (MODE == XENT_STATS || MODE == XENT_PIECE) {
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
           top = fmaxf(top * kLog2e, kLowest);
@@ -157,9 +166,29 @@ struct XentTile {
       }
     };
     const bool inside = n0 + BN <= p.vocab;
+    auto is_plain = [&](int b) LORA_INLINE {
+      return inside && !__any((unsigned)(lds.label[r0 + 16 * b + c16] - c0) < (unsigned)(16 * FA));
+    };
+    if constexpr (MODE == XENT_LOCAL) {   // the tile's own references
+      each_of<FB>([&](auto bc) LORA_INLINE {
+        float top;
+        if (is_plain(decltype(bc)::value)) top = largest(bc, std::true_type{});
+        else top = largest(bc, std::false_type{});
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (g == 0) lds.joined[wn][r0 + 16 * decltype(bc)::value + c16].m = top;
+      });
+      __syncthreads();
+      for (int i = tid; i < BM; i += NT) {
+        float top = lds.joined[0][i].m;
+#pragma unroll
+        for (int w = 1; w < WN; ++w) top = fmaxf(top, lds.joined[w][i].m);
+        lds.ref[i] = ceilf(fmaxf(top * kLog2e, kLowest));
+      }
+      __syncthreads();
+    }
     each_of<FB>([&](auto bc) LORA_INLINE {
-      const int y = lds.label[r0 + 16 * decltype(bc)::value + c16];
-      if (inside && !__any((unsigned)(y - c0) < (unsigned)(16 * FA))) rows_of(bc, std::true_type{});
+      if (is_plain(decltype(bc)::value)) rows_of(bc, std::true_type{});
       else rows_of(bc, std::false_type{});
     });
     if constexpr (MODE != XENT_STATS) tile_to_lds<Core, BN>(acc, lds.stages);
@@ -182,18 +211,20 @@ struct XentTile {
       const size_t at = (size_t)tn * BN;
       lds_to_rows<BM, BN, NT>(lds.stages, p.piece + (size_t)m0 * p.piece_cols + at, (size_t)p.piece_cols, BM, BN);
       if (MODE == XENT_GRAD && p.turned) {
-        for (int e = tid; e < BN * BM / 8; e += NT) {   // 8 rows of a column; 8 neighbours a column's 64 rows
-          const int rb = e & 7, rest = e >> 3, col = rest % BN, r = 64 * (rest / BN) + 8 * rb;
-          int4v v;
-#pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            uint32_t w = 0;
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-              w |= (uint32_t)*reinterpret_cast<const u16*>(lds.stages + tile_at<BN>(r + 2 * h + q, col >> 3) + (col & 7) * 2) << (16 * q);
-            v[h] = (int)w;
-          }
-          *reinterpret_cast<int4v*>(p.turned + (at + col) * p.rows_pad + m0 + r) = v;
+        // A wave turns 32 rows x 16 columns at a time: 16 lanes read 4 rows x 16 columns, lane i
+        // receives column i's, and two such reads are 8 rows of it.
+        constexpr int BLOCKS = (BM / 32) * (BN / 16);
+        static_assert(BLOCKS % NW == 0, "whole waves");
+        const int e4 = c16 >> 2, q4 = c16 & 3;
+#pragma unroll 4
+        for (int i = 0; i < BLOCKS / NW; ++i) {
+          const int blk = wave + NW * i, r = 32 * (blk / (BN / 16)) + 8 * g, col = 16 * (blk % (BN / 16));
+          const int ch = (col >> 3) + (q4 >> 1);
+          int2w lo, hi;
+          read_tr_asm<Bf16, 0>(lo, lds_addr(lds.stages) + tile_at<BN>(r + e4, ch) + (q4 & 1) * 8);
+          read_tr_asm<Bf16, 0>(hi, lds_addr(lds.stages) + tile_at<BN>(r + 4 + e4, ch) + (q4 & 1) * 8);
+          asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(lo), "+v"(hi));
+          *reinterpret_cast<int4v*>(p.turned + (at + col + c16) * p.rows_pad + m0 + r) = int4v{lo.x, lo.y, hi.x, hi.y};
         }
       }
     }
@@ -230,7 +261,12 @@ __global__ __launch_bounds__(NT) void lora_xent_logits_kernel(XentLogits p) {
         const float d = known ? p.dloss[row] : 0.0f;
         lds.ref[i] = known ? p.saved[2 * row] : 0.0f;
         lds.scale[i] = d;
-        lds.own[i] = known ? -d * p.saved[2 * row + 1] : 0.0f;
+        const float o = known ? -d * p.saved[2 * row + 1] : 0.0f;
+        lds.own[i] = o;
+        if (p.coef && tn == 0) {   // what the label's entry of G loses as bf16
+          p.coef[2 * row] = 1.0f;
+          p.coef[2 * row + 1] = o - bf16_to_f32(f32_to_bf16(o));
+        }
       }
     }
     if (MODE == XENT_AGAIN && !__syncthreads_or(again)) continue;
@@ -260,13 +296,14 @@ __device__ __forceinline__ RowEnd row_end(float ref, float others, float zy, boo
 
 // Joins the tiles' parts of RB rows, 256 / RB threads a row, in a fixed order.  The
 // forward keeps lse and rest in `saved` (or nowhere), the one-pass call c1 and c2 in
-// `coef`.
+// `coef` and, with local references, the largest of them in `ref`.
 template <int RB>
 __global__ __launch_bounds__(256) void lora_xent_rows_kernel(const Part* __restrict__ parts, const float* __restrict__ zy,
                                                              const int32_t* __restrict__ labels,
                                                              const float* __restrict__ dloss, float* __restrict__ loss,
-                                                             float* __restrict__ saved, float* __restrict__ coef, int rows,
-                                                             int vocab, int tiles, int64_t rows_pad) {
+                                                             float* __restrict__ saved, float* __restrict__ coef,
+                                                             float* __restrict__ ref, int rows, int vocab, int tiles,
+                                                             int64_t rows_pad) {
   constexpr int PER = 256 / RB;
   __shared__ Part lds[256];
   const int tid = threadIdx.x, r = tid % RB, row = (int)blockIdx.x * RB + r;   // below rows_pad
@@ -290,7 +327,9 @@ __global__ __launch_bounds__(256) void lora_xent_rows_kernel(const Part* __restr
     __syncthreads();
     if (tid / RB < d) add(lds[tid + d * RB]);
   }
-  if (tid >= RB || row >= rows) return;
+  if (tid >= RB) return;
+  if (ref) ref[row] = v.m;
+  if (row >= rows) return;
   const int y = labels[row];
   const bool known = y >= 0 && y < vocab;
   const RowEnd e = row_end(v.m, v.s, known ? zy[row] : 0.0f, known);
@@ -313,13 +352,27 @@ __global__ __launch_bounds__(256) void lora_xent_begin_kernel(float* ref, uint32
   best[i] = ordered(kLowest);
 }
 
+// X for dW: rows without a label are 0 there, whatever they hold (G is, and its product
+// with a NaN would not be).
+__global__ __launch_bounds__(256) void lora_xent_known_kernel(const u16* __restrict__ X, const int32_t* __restrict__ labels,
+                                                              u16* __restrict__ out, int64_t chunks, int per, int vocab) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= chunks) return;
+  const int y = labels[e / per];
+  const int4v v = reinterpret_cast<const int4v*>(X)[e];
+  reinterpret_cast<int4v*>(out)[e] = y >= 0 && y < vocab ? v : int4v{0, 0, 0, 0};
+}
+
 // ---- the second product ----------------------------------------------------------
 struct XentGrad {
   const u16 *A, *B;        // A: [rows of the output][a_cols], B: [contraction][k]
   float* sums;             // [split][tile][fragment][thread][4]: what pieces carry
   bool first, last;        // no sums so far; the result is stored (one split)
   const float *ref_old, *ref;   // the rows' references before and in this piece (or none)
-  const float* coef;       // out = coef[0] sum + coef[1] W_label (or none: the sum)
+  const Part* parts;       // local references: [tile][rows_pad], tiles of 2^tile_log stages
+  int tile_log;
+  int64_t rows_pad;
+  const float* coef;       // out = coef[0] sum + coef[1] W_label, 0 without a label (or none: the sum)
   const int32_t* labels;
   const u16* W;
   u16* out;                // bf16 rows of k
@@ -345,10 +398,12 @@ __device__ __forceinline__ floatx4 with_label(floatx4 v, const float* coef, cons
 // result, or stored with the label's part of the one-pass call.
 enum XentEnd { XENT_CARRY, XENT_STORE, XENT_LABEL };
 
-template <class Core, int BM, int NT, int END>
+// LOCAL: A's tiles have references of their own (parts), and ref is the row's.
+template <class Core, int BM, int NT, int END, bool LOCAL>
 __global__ __launch_bounds__(NT) void lora_xent_grad_kernel(XentGrad p) {
   constexpr int FA = std::extent_v<typename Core::Acc, 0>, FB = std::extent_v<typename Core::Acc, 1>;
-  __shared__ __attribute__((aligned(1024))) char smem[Core::SMEM];
+  constexpr int LT = LOCAL ? local_tiles(BM) : 0;
+  __shared__ __attribute__((aligned(1024))) char smem[Core::SMEM + LT * BM * 2];
   const int tiles = p.tiles_m * p.tiles_n, split = (int)blockIdx.x / tiles;
   int tm, tn;
   tile_coords(p.tiles_m, p.tiles_n, 8, (int)blockIdx.x - split * tiles, tm, tn);
@@ -358,13 +413,24 @@ __global__ __launch_bounds__(NT) void lora_xent_grad_kernel(XentGrad p) {
                  reinterpret_cast<const char*>(p.B + l0), brow, (uint64_t)p.b_rows * brow - (uint64_t)l0 * 2, p.stages};
   typename Core::Acc acc;
   const int s0 = (int)((int64_t)p.stages * split / p.splits), s1 = (int)((int64_t)p.stages * (split + 1) / p.splits);
-  Core::run(t, Scales{}, m0, s0, s1, smem, acc);
+  if constexpr (LOCAL) {
+    u16* table = reinterpret_cast<u16*>(smem + Core::SMEM);   // (read behind the core's barriers)
+    const int first = s0 >> p.tile_log, count = s1 > s0 ? ((s1 - 1) >> p.tile_log) - first + 1 : 0;
+    for (int i = threadIdx.x; i < min(count, LT) * BM; i += NT) {
+      const int row = m0 + i % BM;
+      const float d = p.ref[row] - p.parts[(size_t)(first + i / BM) * p.rows_pad + row].m;
+      table[i] = d < 255.0f ? (u16)((int)d << 7) : (u16)(255 << 7);   // (a NaN: 255, and the row's result is one)
+    }
+    Core::template run<true>(t, Scales{}, m0, s0, s1, smem, acc, Shifts<BM>{table, first, p.tile_log});
+  } else {
+    Core::run(t, Scales{}, m0, s0, s1, smem, acc);
+  }
   const int lane = lane_fresh(), wave = uniform((int)threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
   floatx4* to = reinterpret_cast<floatx4*>(p.sums) + ((size_t)split * tiles + (size_t)tm * p.tiles_n + tn) * (FA * FB * NT) + threadIdx.x;
 #pragma unroll
   for (int b = 0; b < FB; ++b) {
     const int row = m0 + Core::row0(wave) + 16 * b + c16;
-    const float alpha = !p.first && p.ref ? __builtin_amdgcn_exp2f(p.ref_old[row] - p.ref[row]) : 1.0f;
+    const float alpha = !LOCAL && !p.first && p.ref ? __builtin_amdgcn_exp2f(p.ref_old[row] - p.ref[row]) : 1.0f;
 #pragma unroll
     for (int a = 0; a < FA; ++a) {
       floatx4 v = acc[a][b];
@@ -437,10 +503,19 @@ using Grad256 = NnBig<Bf16>;
 template <int END>
 static hipError_t run_grad_of(int kind, const XentGrad& q, hipStream_t st) {
   const dim3 grid((unsigned)(q.tiles_m * q.tiles_n * q.splits));
+  if constexpr (END != XENT_STORE) {
+    if (q.parts) {
+      if (kind == XENT_GRAD_64x256)
+        hipLaunchKernelGGL((lora_xent_grad_kernel<Grad64, 64, 256, END, true>), grid, dim3(256), 0, st, q);
+      else
+        hipLaunchKernelGGL((lora_xent_grad_kernel<Grad128, 128, 512, END, true>), grid, dim3(512), 0, st, q);
+      return hipGetLastError();
+    }
+  }
   switch (kind) {
-    case XENT_GRAD_64x256: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad64, 64, 256, END>), grid, dim3(256), 0, st, q); break;
-    case XENT_GRAD_128x256: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad128, 128, 512, END>), grid, dim3(512), 0, st, q); break;
-    default: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad256, 256, 512, END>), grid, dim3(512), 0, st, q);
+    case XENT_GRAD_64x256: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad64, 64, 256, END, false>), grid, dim3(256), 0, st, q); break;
+    case XENT_GRAD_128x256: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad128, 128, 512, END, false>), grid, dim3(512), 0, st, q); break;
+    default: hipLaunchKernelGGL((lora_xent_grad_kernel<Grad256, 256, 512, END, false>), grid, dim3(512), 0, st, q);
   }
   return hipGetLastError();
 }
@@ -500,33 +575,45 @@ struct XentCall {
     g.tiles_m = p.grad_tiles_m; g.tiles_n = p.tiles_k; g.splits = p.splits;   // (some have nothing but their scaling to do in a short last piece)
     return g;
   }
-  hipError_t rows(float* saved, float* coef) const {
+  hipError_t rows(float* saved, float* coef, float* ref) const {
     const Part* parts = at<Part>(L.parts);
     const float* zy = at<float>(L.zy);
     if (a.rows <= 1024)
       hipLaunchKernelGGL((lora_xent_rows_kernel<4>), dim3((unsigned)cdiv(a.rows, 4)), dim3(256), 0, st, parts, zy, a.labels,
-                         a.dloss, a.loss, saved, coef, (int)a.rows, (int)a.vocab, p.vtiles, p.rows_pad);
+                         a.dloss, a.loss, saved, coef, ref, (int)a.rows, (int)a.vocab, p.vtiles, p.rows_pad);
     else
       hipLaunchKernelGGL((lora_xent_rows_kernel<16>), dim3((unsigned)cdiv(a.rows, 16)), dim3(256), 0, st, parts, zy, a.labels,
-                         a.dloss, a.loss, saved, coef, (int)a.rows, (int)a.vocab, p.vtiles, p.rows_pad);
+                         a.dloss, a.loss, saved, coef, ref, (int)a.rows, (int)a.vocab, p.vtiles, p.rows_pad);
     return hipGetLastError();
   }
   hipError_t forward(float* saved) const {
     LORA_TRY(run_logits<XENT_STATS>(p, logits(), st));
-    return rows(saved, nullptr);
+    return rows(saved, nullptr, nullptr);
   }
   hipError_t backward(const float* saved) const {
     XentLogits q = logits();
     q.saved = saved;
     q.turned = a.dW ? at<u16>(L.turned) : nullptr;
+    float* coef = at<float>(L.coef);
+    if (a.dW) {
+      const int64_t chunks = a.rows * (a.k / 8);
+      hipLaunchKernelGGL(lora_xent_known_kernel, dim3((unsigned)cdiv(chunks, 256)), dim3(256), 0, st, a.X, a.labels,
+                         at<u16>(L.known), chunks, (int)(a.k / 8), (int)a.vocab);
+      LORA_TRY(hipGetLastError());
+    }
     for (int i = 0; i < p.pieces; ++i) {
       at_piece(q, i);
+      q.coef = i == 0 && a.dX ? coef : nullptr;
       LORA_TRY(run_logits<XENT_GRAD>(p, q, st));
-      if (a.dX) LORA_TRY(run_grad(p.grad_kind, dx(i), st));
+      if (a.dX) {
+        XentGrad g = dx(i);
+        g.coef = coef;
+        LORA_TRY(run_grad(p.grad_kind, g, st));
+      }
       if (a.dW) {
         const int64_t v0 = i * p.piece, cols = std::min(p.piece, a.vocab - v0);
         XentGrad g{};
-        g.A = q.turned; g.B = a.X; g.out = a.dW + v0 * a.k;
+        g.A = q.turned; g.B = at<u16>(L.known); g.out = a.dW + v0 * a.k;
         g.a_cols = p.rows_pad; g.b_rows = a.rows;
         g.first = g.last = true;
         g.m = g.rows = (int)cols; g.k = (int)a.k;
@@ -535,7 +622,10 @@ struct XentCall {
         LORA_TRY(run_grad(XENT_GRAD_256x256, g, st));
       }
     }
-    return a.dX && p.splits > 1 ? run_join(p.grad_kind, dx(0), st) : hipSuccess;
+    if (!a.dX || p.splits == 1) return hipSuccess;
+    XentGrad g = dx(0);
+    g.coef = coef;
+    return run_join(p.grad_kind, g, st);
   }
   // Loss and dX, the logits formed once.
   hipError_t one_pass() const {
@@ -543,6 +633,19 @@ struct XentCall {
     float* ref[2] = {at<float>(L.ref), at<float>(L.ref) + p.rows_pad};
     uint32_t* best[2] = {at<uint32_t>(L.best), at<uint32_t>(L.best) + p.rows_pad};
     float* coef = at<float>(L.coef);
+    if (p.local) {
+      at_piece(q, 0);
+      LORA_TRY(run_logits<XENT_LOCAL>(p, q, st));
+      LORA_TRY(rows(nullptr, coef, ref[0]));
+      XentGrad g = dx(0);
+      g.coef = coef;
+      g.ref = ref[0];
+      g.parts = q.parts;
+      g.tile_log = p.tile_n == 256 ? 2 : 1;
+      g.rows_pad = p.rows_pad;
+      LORA_TRY(run_grad(p.grad_kind, g, st));
+      return p.splits == 1 ? hipSuccess : run_join(p.grad_kind, g, st);
+    }
     hipLaunchKernelGGL(lora_xent_begin_kernel, dim3((unsigned)cdiv(p.rows_pad, 256)), dim3(256), 0, st, ref[0], best[0],
                        p.rows_pad);
     LORA_TRY(hipGetLastError());
@@ -555,7 +658,7 @@ struct XentCall {
       LORA_TRY(run_logits<XENT_PIECE>(p, q, st));
       LORA_TRY(run_logits<XENT_AGAIN>(p, q, st));
       XentGrad g = dx(i);
-      if (i + 1 == p.pieces) LORA_TRY(rows(nullptr, coef));
+      if (i + 1 == p.pieces) LORA_TRY(rows(nullptr, coef, nullptr));
       if (g.last) g.coef = coef;
       g.ref_old = q.ref;
       g.ref = q.ref_next;

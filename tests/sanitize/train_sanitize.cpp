@@ -108,15 +108,19 @@ static int plans() {
         HOLDS(p.piece == (int64_t)p.piece_tiles * p.tile_n && p.piece % 64 == 0 && p.stages * 64 == p.piece, rows, vocab, k);
         HOLDS((int64_t)p.tiles_m * p.vtiles < (int64_t(1) << 31) && (int64_t)p.grad_tiles_m * p.tiles_k * p.splits < (int64_t(1) << 28), rows, vocab, k);
         HOLDS(p.splits >= 1, rows, vocab, k);
+        for (int64_t sp = 0; p.local && sp < p.splits; ++sp) {   // the tiles of logits that a part of the contraction meets
+          const int64_t s0 = p.stages * sp / p.splits, s1 = p.stages * (sp + 1) / p.splits, per = p.tile_n / 64;
+          HOLDS(s1 <= s0 || (s1 - 1) / per - s0 / per + 1 <= local_tiles(p.grad_m), rows, vocab, k);
+        }
         // what the tiles' 32-bit offsets reach: 256 rows of each operand
         HOLDS(p.piece * 2 * p.tile_m < (int64_t(1) << 31) && p.rows_pad * 2 * 256 < (int64_t(1) << 31) && k * 2 * 256 < (int64_t(1) << 31), rows, vocab, k);
         size_t last = 0;
         for (int d = 0; d < 4; ++d) {
           const XentLayout L = xent_layout(rows, vocab, k, d & 1, d >> 1);
-          HOLDS(L.coef - L.zy >= (size_t)p.rows_pad * 4 && L.ref - L.coef >= (size_t)p.rows_pad * 8 && L.best - L.ref >= (size_t)p.rows_pad * 8 && L.parts - L.best >= (size_t)p.rows_pad * 8 && L.parts <= L.piece && L.piece <= L.turned && L.turned <= L.sums && L.sums <= L.saved && L.saved <= L.total, rows, vocab, k);
+          HOLDS(L.coef - L.zy >= (size_t)p.rows_pad * 4 && L.ref - L.coef >= (size_t)p.rows_pad * 8 && L.best - L.ref >= (size_t)p.rows_pad * 8 && L.parts - L.best >= (size_t)p.rows_pad * 8 && L.parts <= L.piece && L.piece <= L.turned && L.turned <= L.known && L.known <= L.sums && L.sums <= L.saved && L.saved <= L.total, rows, vocab, k);
           HOLDS(L.piece - L.parts >= (size_t)(p.vtiles * p.rows_pad * 8), rows, vocab, k);
           if (d) HOLDS(L.turned - L.piece >= (size_t)(p.rows_pad * p.piece * 2), rows, vocab, k);
-          if (d & 2) HOLDS(L.sums - L.turned >= (size_t)(p.rows_pad * p.piece * 2) && L.total - L.saved >= (size_t)(rows * 8), rows, vocab, k);
+          if (d & 2) HOLDS(L.known - L.turned >= (size_t)(p.rows_pad * p.piece * 2) && L.sums - L.known >= (size_t)(rows * k * 2) && L.total - L.saved >= (size_t)(rows * 8), rows, vocab, k);
           if (d & 1) HOLDS(L.saved - L.sums >= (size_t)p.splits * p.grad_tiles_m * p.grad_m * p.tiles_k * 256 * 4, rows, vocab, k);
           if (d != 2) HOLDS(L.total >= last, rows, vocab, k);   // a call with fewer outputs needs no more
           last = d == 2 ? last : L.total;
@@ -132,7 +136,7 @@ int main(int argc, char** argv) {
       const int64_t m = atoll(argv[i]), n = atoll(argv[i + 1]), k = atoll(argv[i + 2]);
       if (strcmp(argv[1], "xent") == 0) {   // rows, vocab, k: its kernels, and whether there are parts to join and pieces
         const lora::XentPlan p = lora::plan_xent(m, n, k);
-        printf("logits%d grad%d join%d pieces%d\n", p.kind, p.grad_kind, p.splits > 1 ? p.grad_kind : -1, p.pieces > 1);
+        printf("logits%d grad%d join%d pieces%d local%d\n", p.kind, p.grad_kind, p.splits > 1 ? p.grad_kind : -1, p.pieces > 1, p.local ? p.grad_kind : -1);
         continue;
       }
       printf("%d\n", (int)(strcmp(argv[1], "fwd") == 0 ? lora::plan_fp8_fwd(m, n, k) : lora::plan_fp8_bwd(m, n, k)).kind);

@@ -93,7 +93,7 @@ def close(got, want, tol, label=""):
 SIZES = [(1, 1, 8), (1, 2, 64), (1, 32000, 512), (2, 129, 40), (5, 1000, 264), (16, 128, 64), (37, 5001, 520), (63, 127, 72),
          (64, 257, 128), (65, 4000, 256), (100, 333, 1032), (128, 2048, 512), (129, 300, 64), (130, 1023, 200), (200, 10007, 136),
          (256, 256, 64), (257, 257, 328), (300, 5000, 512), (513, 2049, 72), (700, 1500, 264), (1000, 8003, 64), (1500, 769, 512),
-         (90, 16000, 2056), (200, 20000, 1024), (250, 9001, 2048), (600, 4000, 1032), (1030, 2000, 72), (2060, 3000, 264), (4100, 1000, 4104), (1000, 15000, 4104)]
+         (90, 16000, 2056), (200, 20000, 1024), (250, 9001, 2048), (600, 4000, 1032), (1030, 2000, 72), (2060, 3000, 264), (4100, 1000, 4104), (1000, 15000, 4104), (384, 5000, 4104), (2000, 9000, 1032)]
 
 
 @pytest.mark.parametrize("rows,vocab,k", SIZES)
@@ -167,6 +167,12 @@ def test_not_a_number(rows):
         assert np.isnan(loss[:3]).all() and np.isnan(dX[:3]).all(), how
         assert (loss[3:5] == 0).all() and (dX[3:5] == 0).all(), how
         assert np.isfinite(loss[5:]).all() and np.isfinite(dX[5:]).all(), how
+    labels[:3] = [-1, vocab, -100]                            # padding may hold anything
+    clean = x.copy()
+    clean[:5] = 0
+    for how in ("step", "two"):
+        got, want = run(x, w, labels, d, how, True, True), run(clean, w, labels, d, how, True, True)
+        assert all(np.array_equal(a, b) for a, b in zip(got, want)), how
 
 
 def test_no_labels_at_all():
