@@ -161,7 +161,10 @@ struct BScales {
 // A compute unit often holds one such workgroup, a wave to a SIMD, and then the wave's
 // own instructions bound a stage: the loop is unrolled over the stages' places, whose
 // addresses are constants, and copies past the end take the last stage again (nobody
-// reads them) instead of a condition each.
+// reads them) instead of a condition each.  Copies and LDS reads are issued between the
+// products, a few behind each row fragment's: issued ahead of them all they took 0.1 us
+// more of a stage (8 bits, 256 x 128: 0.58 to 0.90 us against 0.77 to 1.00; 1531 x 4104
+// x 3208 27.5 -> 24.2 us), since the wave's first product waited for its last issue.
 template <class E, int BM, int BN, int WM, int WN, int NS, bool TAIL>
 struct NtCore {
   static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FA = TN / 16, FB = TM / 16;
@@ -198,19 +201,21 @@ struct NtCore {
     const uint32_t last = (uint32_t)(t.stages - 1) * 128, slast = (uint32_t)(t.stages - 1) * sstep;
     uint32_t at = 0, sat = 0;   // of the next stage to copy
     char* const mine = smem + crow * 128;
-    auto copy = [&](auto place) LORA_INLINE {
-      char* sb = mine + decltype(place)::value * STAGE;
+    // The q-th copy of the wave's C of a stage; the last one moves on to the next stage.
+    auto copy_one = [&](auto place, auto qc) LORA_INLINE {
+      constexpr int Q = decltype(qc)::value, O = decltype(place)::value * STAGE;
       const bool out = TAIL && at + kcol >= t.kbytes;
-#pragma unroll
-      for (int i = 0; i < CX; ++i) dma16(t.a, out ? kOOB : aoff[i], at, sb + 8 * NW * i * 128);
-#pragma unroll
-      for (int i = 0; i < CB; ++i) dma16(t.b, out ? kOOB : boff[i], at, sb + (BM + 8 * NW * i) * 128);
-      if constexpr (E::SCALED) {
-        dma4(rsS, soff, sat, smem + decltype(place)::value * STAGE + SOFF + wave * 256);
+      if constexpr (Q < CX) {
+        dma16(t.a, out ? kOOB : aoff[Q], at, mine + O + 8 * NW * Q * 128);
+      } else if constexpr (Q < CX + CB) {
+        dma16(t.b, out ? kOOB : boff[Q - CX], at, mine + O + (BM + 8 * NW * (Q - CX)) * 128);
+      } else {
+        dma4(rsS, soff, sat, smem + O + SOFF + wave * 256);
         sat = min(sat + sstep, slast);
       }
-      at = min(at + 128, last);
+      if constexpr (Q == C - 1) at = min(at + 128, last);
     };
+    auto copy = [&](auto place) LORA_INLINE { each_of<C>([&](auto q) LORA_INLINE { copy_one(place, q); }); };
     Frag fa[2][FA], fb[2][FB];   // of this stage and the next
     int sa[2] = {}, sw[2][TM / 64] = {};
     // Rows 16 apart swizzle alike, and the second chunk is 4 further.
@@ -218,36 +223,50 @@ struct NtCore {
     const char *a0 = smem + (BM + wn * TN) * 128 + f0, *a1 = smem + (BM + wn * TN) * 128 + f1;
     const char *b0 = smem + wm * TM * 128 + f0, *b1 = smem + wm * TM * 128 + f1;
     const char* s0 = smem + SOFF + wave * 256 + c16 * 4;
-    auto read = [&](int kb, auto place, auto set) LORA_INLINE {
+    int O = 0;   // of the place that is read
+    auto read_scales = [&](int kb, auto set) LORA_INLINE {
       constexpr int S = decltype(set)::value;
-      int O = decltype(place)::value * STAGE;
-      // Addresses beyond the reads' own offsets are formed here where a wave's sums need the
-      // registers that keeping them for every place takes.
-      if (SMEM > 65536 && FA * FB >= 16) asm volatile("" : "+s"(O));
       if constexpr (E::SCALED) {
         sa[S] = bs.at(kb, 0);
 #pragma unroll
         for (int i = 0; i < TM / 64; ++i) sw[S][i] = *reinterpret_cast<const int*>(s0 + O + i * 64);
       }
-#pragma unroll
-      for (int a = 0; a < FA; ++a)
-        fa[S][a] = Frag{*reinterpret_cast<const int4v*>(a0 + O + 2048 * a), *reinterpret_cast<const int4v*>(a1 + O + 2048 * a)};
-#pragma unroll
-      for (int b = 0; b < FB; ++b)
-        fb[S][b] = Frag{*reinterpret_cast<const int4v*>(b0 + O + 2048 * b), *reinterpret_cast<const int4v*>(b1 + O + 2048 * b)};
     };
-    auto multiply = [&](auto set) LORA_INLINE {
+    auto read_one = [&](auto set, auto qc) LORA_INLINE {   // fragment q of the FA + FB
+      constexpr int S = decltype(set)::value, Q = decltype(qc)::value;
+      if constexpr (Q < FA)
+        fa[S][Q] = Frag{*reinterpret_cast<const int4v*>(a0 + O + 2048 * Q), *reinterpret_cast<const int4v*>(a1 + O + 2048 * Q)};
+      else
+        fb[S][Q - FA] = Frag{*reinterpret_cast<const int4v*>(b0 + O + 2048 * (Q - FA)),
+                             *reinterpret_cast<const int4v*>(b1 + O + 2048 * (Q - FA))};
+    };
+    auto set_place = [&](auto place) LORA_INLINE {
+      O = decltype(place)::value * STAGE;
+      // Addresses beyond the reads' own offsets are formed here where a wave's sums need the
+      // registers that keeping them for every place takes.
+      if (SMEM > 65536 && FA * FB >= 16) asm volatile("" : "+s"(O));
+    };
+    // A stage's products; behind each row fragment's, f(its index).
+    auto multiply = [&](auto set, auto&& f) LORA_INLINE {
       constexpr int S = decltype(set)::value;
       each_of<FB>([&](auto bc) LORA_INLINE {
         constexpr int B = decltype(bc)::value;
 #pragma unroll
         for (int a = 0; a < FA; ++a)
           acc[a][B] = stage_product<E, B & 3>(fa[S][a], fb[S][B], acc[a][B], sa[S], sw[S][B >> 2]);
+        __builtin_amdgcn_sched_barrier(0);
+        f(bc);
+        __builtin_amdgcn_sched_barrier(0);
       });
     };
     each_of<NS>([&](auto j) LORA_INLINE { copy(j); });
     copy_barrier<(NS - 1) * C>();
-    read(0, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+    {
+      using I0 = std::integral_constant<int, 0>;
+      set_place(I0{});
+      read_scales(0, I0{});
+      each_of<FA + FB>([&](auto q) LORA_INLINE { read_one(I0{}, q); });
+    }
     constexpr int U = NS % 2 ? 2 * NS : NS;
     for (int k0 = 0; k0 < t.stages; k0 += U) {
       if constexpr (E::SCALED)
@@ -255,12 +274,25 @@ struct NtCore {
       each_of<U>([&](auto jc) LORA_INLINE {
         constexpr int J = decltype(jc)::value;
         // The next stage has landed, and every wave has read this one, whose place is
-        // filled again; the next one's fragments are read under this one's products.
+        // filled again.  The products come first; copies and the next stage's reads are
+        // issued between them.
         if (J == 0 || k0 + J < t.stages) {
+          using Next = std::integral_constant<int, (J + 1) & 1>;
           copy_barrier<(NS - 2) * C>();
-          copy(std::integral_constant<int, J % NS>{});
-          read(k0 + J + 1, std::integral_constant<int, (J + 1) % NS>{}, std::integral_constant<int, (J + 1) & 1>{});
-          multiply(std::integral_constant<int, J & 1>{});
+          __builtin_amdgcn_sched_barrier(0);
+          multiply(std::integral_constant<int, J & 1>{}, [&](auto bc) LORA_INLINE {
+            constexpr int B = decltype(bc)::value;
+            if constexpr (B == 0) {
+              set_place(std::integral_constant<int, (J + 1) % NS>{});
+              read_scales(k0 + J + 1, Next{});
+            }
+            each_of<FA + FB>([&](auto q) LORA_INLINE {
+              if constexpr (decltype(q)::value * FB / (FA + FB) == B) read_one(Next{}, q);
+            });
+            each_of<C>([&](auto q) LORA_INLINE {
+              if constexpr (decltype(q)::value * FB / C == B) copy_one(std::integral_constant<int, J % NS>{}, q);
+            });
+          });
         }
       });
     }
@@ -324,7 +356,8 @@ struct Shifts {
   __device__ __forceinline__ uint32_t at(int stage, int row) const { return table[((stage >> log) - first) * ROWS + row]; }
 };
 
-// C = A B, BM x BN (BN 128 or 256) by WM x WN waves, NS stages.
+// C = A B, BM x BN (BN 256) by WM x WN waves, NS stages, issued as in NtCore (8 bits,
+// 2048 x 4096 x 4096 on 128 x 256: 36.8 -> 34.4 us).
 template <class E, int BM, int BN, int WM, int WN, int NS>
 struct NnCore {
   static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FA = TN / 16, FB = TM / 16;
@@ -370,20 +403,25 @@ struct NnCore {
     uint32_t at = (uint32_t)s0 * 128, sat = (uint32_t)s0 * sstep;   // of the next stage to copy
     NnRows rows;
     rows.start(t, s0, E::KS);
-    auto copy = [&](auto place) LORA_INLINE {
+    __amdgpu_buffer_rsrc_t rs = t.a;   // B's rows of the stage being copied
+    auto copy_one = [&](auto place, auto qc) LORA_INLINE {   // as in NtCore
+      constexpr int Q = decltype(qc)::value;
       char* sb = smem + decltype(place)::value * STAGE;
-#pragma unroll
-      for (int i = 0; i < CX; ++i) dma16(t.a, aoff[i], at, sb + (crow + 8 * NW * i) * 128);
-      const __amdgpu_buffer_rsrc_t rs = rows.rows();
-#pragma unroll
-      for (int i = 0; i < CB; ++i) dma16(rs, boff[i], 0, sb + BM * 128 + (wave + NW * i) * 1024);
-      if constexpr (E::SCALED) {
+      if constexpr (Q == 0) rs = rows.rows();
+      if constexpr (Q < CX) {
+        dma16(t.a, aoff[Q], at, sb + (crow + 8 * NW * Q) * 128);
+      } else if constexpr (Q < CX + CB) {
+        dma16(rs, boff[Q - CX], 0, sb + BM * 128 + (wave + NW * (Q - CX)) * 1024);
+      } else {
         dma4(rsS, soff, sat, sb + SOFF + wave * 256);
         sat = min(sat + sstep, slast);
       }
-      at = min(at + 128, last);
-      rows.next();
+      if constexpr (Q == C - 1) {
+        at = min(at + 128, last);
+        rows.next();
+      }
     };
+    auto copy = [&](auto place) LORA_INLINE { each_of<C>([&](auto q) LORA_INLINE { copy_one(place, q); }); };
     uint32_t wa[FA];
 #pragma unroll
     for (int a = 0; a < FA; ++a) {
@@ -397,26 +435,26 @@ struct NnCore {
     static_assert(FA == 4, "the wait's operands");
     const uint32_t f0 = kc_offset(c16, g), f1 = f0 ^ 64;
     const char *b0 = smem + wm * TM * 128 + f0, *b1 = smem + wm * TM * 128 + f1;
-    auto read = [&](int kb, auto place, auto set) LORA_INLINE {
+    auto read_scales = [&](int kb, auto place, auto set) LORA_INLINE {
       constexpr int S = decltype(set)::value, O = decltype(place)::value * STAGE;
       if constexpr (E::SCALED) {
         sa[S] = bs.at(kb, 0);
         sw[S] = *reinterpret_cast<const int*>(smem + O + SOFF + wave * 256 + c16 * 4);
       }
-#pragma unroll
-      for (int b = 0; b < FB; ++b)
-        fb[S][b] = Frag{*reinterpret_cast<const int4v*>(b0 + O + 2048 * b), *reinterpret_cast<const int4v*>(b1 + O + 2048 * b)};
       if constexpr (SHIFT)
 #pragma unroll
         for (int b = 0; b < FB; ++b) down[S][b] = shifts.at(min(kb, s1 - 1), wm * TM + 16 * b + c16);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int a = 0; a < FA; ++a) {
-        const uint32_t from = wa[a] + (uint32_t)O;
-        read_tr_asm<E, 0>(w[S][a][0], from);
-        read_tr_asm<E, 1024>(w[S][a][1], from);
-        read_tr_asm<E, 8192>(w[S][a][2], from);
-        read_tr_asm<E, 9216>(w[S][a][3], from);
+    };
+    auto read_one = [&](auto place, auto set, auto qc) LORA_INLINE {   // fragment q of the FB + FA
+      constexpr int S = decltype(set)::value, O = decltype(place)::value * STAGE, Q = decltype(qc)::value;
+      if constexpr (Q < FB) {
+        fb[S][Q] = Frag{*reinterpret_cast<const int4v*>(b0 + O + 2048 * Q), *reinterpret_cast<const int4v*>(b1 + O + 2048 * Q)};
+      } else {
+        const uint32_t from = wa[Q - FB] + (uint32_t)O;
+        read_tr_asm<E, 0>(w[S][Q - FB][0], from);
+        read_tr_asm<E, 1024>(w[S][Q - FB][1], from);
+        read_tr_asm<E, 8192>(w[S][Q - FB][2], from);
+        read_tr_asm<E, 9216>(w[S][Q - FB][3], from);
       }
     };
     auto arrived = [&](auto set) LORA_INLINE {   // (before any branch)
@@ -428,7 +466,7 @@ struct NnCore {
                      "+v"(w[S][3][3]));
       __builtin_amdgcn_sched_barrier(0);
     };
-    auto multiply = [&](auto set) LORA_INLINE {
+    auto multiply = [&](auto set, auto&& issue) LORA_INLINE {
       constexpr int S = decltype(set)::value;
       each_of<FB>([&](auto bc) LORA_INLINE {
         constexpr int B = decltype(bc)::value;
@@ -440,12 +478,16 @@ struct NnCore {
           f.hi = int4v{w[S][a][2].x, w[S][a][2].y, w[S][a][3].x, w[S][a][3].y};
           acc[a][B] = stage_product<E, B & 3>(f, fb[S][B], acc[a][B], sa[S], sw[S]);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        issue(bc);
+        __builtin_amdgcn_sched_barrier(0);
       });
     };
     using I0 = std::integral_constant<int, 0>;
     each_of<NS>([&](auto j) LORA_INLINE { copy(j); });
     copy_barrier<(NS - 1) * C>();
-    read(s0, I0{}, I0{});
+    read_scales(s0, I0{}, I0{});
+    each_of<FA + FB>([&](auto q) LORA_INLINE { read_one(I0{}, I0{}, q); });
     arrived(I0{});
     constexpr int U = NS % 2 ? 2 * NS : NS;
     for (int k0 = s0; k0 < s1; k0 += U) {
@@ -456,10 +498,18 @@ struct NnCore {
         using Next = std::integral_constant<int, (J + 1) & 1>;
         if (J == 0 || k0 + J < s1) {
           copy_barrier<(NS - 2) * C>();
-          copy(std::integral_constant<int, J % NS>{});
-          read(k0 + J + 1, std::integral_constant<int, (J + 1) % NS>{}, Next{});
-          multiply(std::integral_constant<int, J & 1>{});
           __builtin_amdgcn_sched_barrier(0);
+          multiply(std::integral_constant<int, J & 1>{}, [&](auto bc) LORA_INLINE {
+            constexpr int B = decltype(bc)::value;
+            using From = std::integral_constant<int, (J + 1) % NS>;
+            if constexpr (B == 0) read_scales(k0 + J + 1, From{}, Next{});
+            each_of<FA + FB>([&](auto q) LORA_INLINE {
+              if constexpr (decltype(q)::value * FB / (FA + FB) == B) read_one(From{}, Next{}, q);
+            });
+            each_of<C>([&](auto q) LORA_INLINE {
+              if constexpr (decltype(q)::value * FB / C == B) copy_one(std::integral_constant<int, J % NS>{}, q);
+            });
+          });
           arrived(Next{});
         }
       });

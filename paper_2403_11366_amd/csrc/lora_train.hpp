@@ -76,24 +76,24 @@ struct Fp8Plan {
 // out: a round of workgroups that fills the compute units takes c + full x stages, one
 // of few of them c + light x stages, the last one in between.
 //   Forward, fitted to k = 2048 to 11008 (us): 64 x 4096 x 4096 9.9 on 64 x 64 (14.6 on
-// 64 x 128, 15.0 from memory), 24 x 32000 x 4096 21.8 on both, 128 x 11008 x 4096 18.2
-// on 64 x 128 (21 on 64 x 64), 1024 x 4096 x 4096 22.4 on 128 x 128 (28 on 64 x 128, 32
-// on 256 x 128), 1531 x 4104 x 3208 26.7 on 256 x 128 (32 on 128 x 128, 35 on 256 x
-// 256), 4096 x 4096 x 4096 53 on 256 x 256 (69 on 256 x 128).
-//   Backward: 200 x 4096 x 4096 25 on 64 x 256, 17 with four workgroups to a tile, 1024
-// x 4096 x 4096 28.5 on 64 x 256 (35 on 128 x 256, 43 on 256 x 256), 2048 x 4096 x 4096
-// 37 on 128 x 256 (47, 55), 1024 x 4096 x 11008 49 on 256 x 256 (68 on 128 x 256).
+// 64 x 128, 15.0 from memory), 24 x 32000 x 4096 21.8 on both, 128 x 11008 x 4096 18.1
+// on 64 x 128 (21 on 64 x 64, 22 on 128 x 128), 1024 x 4096 x 4096 22.4 on 128 x 128 (28
+// on 64 x 128, 29 on 256 x 128), 1531 x 4104 x 3208 24.7 on 256 x 128 (33 on 128 x 128,
+// 36 on 256 x 256), 4096 x 4096 x 4096 54 on 256 x 256 (63 on 256 x 128).
+//   Backward: 200 x 4096 x 4096 23 on 64 x 256, 17 with four workgroups to a tile, 1024
+// x 4096 x 4096 27.8 on 64 x 256 (30 on 128 x 256, 43 on 256 x 256), 2048 x 4096 x 4096
+// 34.5 on 128 x 256 (53, 47), 1024 x 4096 x 11008 47 on 256 x 256 (60 on 128 x 256).
 struct TileCost {
   int kind, bm, bn, block;
   double c, light, full;
 };
 constexpr TileCost kFp8Tiles[5] = {{FP8_64x64, 64, 64, 256, 1.5, 0.26, 0.29},
                                    {FP8_64x128, 64, 128, 256, 1.8, 0.40, 0.42},
-                                   {FP8_128x128, 128, 128, 512, 2.5, 0.49, 0.62},
-                                   {FP8_256x128, 256, 128, 512, 4.0, 0.77, 1.00},
+                                   {FP8_128x128, 128, 128, 512, 2.5, 0.42, 0.60},
+                                   {FP8_256x128, 256, 128, 512, 4.0, 0.58, 0.90},
                                    {FP8_256x256, 256, 256, 512, 6.0, 1.03, 1.45}};
-constexpr TileCost kFp8BackTiles[3] = {{FP8_BACK_64x256, 64, 256, 256, 2.5, 0.71, 0.80},
-                                       {FP8_BACK_128x256, 128, 256, 512, 3.5, 0.80, 1.02},
+constexpr TileCost kFp8BackTiles[3] = {{FP8_BACK_64x256, 64, 256, 256, 2.5, 0.62, 0.77},
+                                       {FP8_BACK_128x256, 128, 256, 512, 3.5, 0.70, 0.96},
                                        {FP8_BACK_256x256, 256, 256, 512, 6.0, 1.03, 1.65}};
 inline double tile_time(const TileCost& t, int64_t grid, double stages) {
   const int64_t rounds = cdiv(grid, 256), last = grid - (rounds - 1) * 256;
@@ -204,15 +204,21 @@ struct XentArgs {
 };
 
 // The logits' tiles and those of dX, by estimated time (TileCost above; a stage of 64
-// bf16 columns moves and multiplies as much as one of 128 8-bit ones).
+// bf16 columns moves as much as one of 128 8-bit ones).  Measured, rows x vocabulary x k:
+// the loss alone (us) 300 x 4000 x 1024 13.0 on 64 x 128 (14.3 on 128 x 128, 20, 31), 37
+// x 32000 x 4096 43 on 64 x 128 (50 on 256 x 128), 200 x 32000 x 4096 61 on 256 x 128
+// (74 on 128 x 128, 82 on 256 x 256, 103 on 64 x 128), 1024 x 32000 x 4096 197 on 256 x
+// 256 (230 on 256 x 128).  Loss with dX: 200 x 32000 x 4096 172 on 64 x 256 shared by
+// four workgroups (176 on 128 x 256, 216 on 256 x 256, 383 unshared), 512 x 32003 x 4096
+// 249 on 256 x 256 shared by eight (262 on 128 x 256 by four, 311 on 64 x 256).
 enum XentTileKind { XENT_64x128, XENT_128x128, XENT_256x128, XENT_256x256 };
 enum XentGradKind { XENT_GRAD_64x256, XENT_GRAD_128x256, XENT_GRAD_256x256 };
 constexpr TileCost kXentTiles[4] = {{XENT_64x128, 64, 128, 256, 3.0, 0.45, 0.62},
-                                    {XENT_128x128, 128, 128, 512, 5.0, 0.50, 0.65},
-                                    {XENT_256x128, 256, 128, 512, 7.0, 0.78, 1.02},
+                                    {XENT_128x128, 128, 128, 512, 5.0, 0.45, 0.60},
+                                    {XENT_256x128, 256, 128, 512, 7.0, 0.65, 0.90},
                                     {XENT_256x256, 256, 256, 512, 11.0, 1.03, 1.35}};
-constexpr TileCost kXentGradTiles[3] = {{XENT_GRAD_64x256, 64, 256, 256, 2.5, 0.71, 0.80},
-                                        {XENT_GRAD_128x256, 128, 256, 512, 4.5, 0.80, 0.93},
+constexpr TileCost kXentGradTiles[3] = {{XENT_GRAD_64x256, 64, 256, 256, 2.5, 0.66, 0.77},
+                                        {XENT_GRAD_128x256, 128, 256, 512, 4.5, 0.72, 0.88},
                                         {XENT_GRAD_256x256, 256, 256, 512, 6.0, 1.03, 1.45}};
 
 // The vocabulary is walked in pieces: the exponentials (or gradients) of a piece's
