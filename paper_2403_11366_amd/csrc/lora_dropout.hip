@@ -5,34 +5,33 @@
 // packed masks hold the same bits), is below floor((1 - p) 2^16 + 1/2).  The
 // gradient is the same call on dY without the residual.
 //
-// A thread makes the 16 elements of a block.
+// A thread draws a block.  bf16: it takes the block's 32 bytes.  fp32: its 64 bytes
+// would leave lanes' loads 64 bytes apart; through LDS each lane gets the draws of four
+// 16-byte pieces instead, a load of the wave's being one run of 1 KiB (8192 x 4096: 60.8
+// -> 46.7 us, with a residual 82 -> 71; for bf16 the detour costs: 25.4 and 26.8).  Bounded by
+// memory where there is much of it -- 8192 x 4096 bf16 with a residual 35.8 us, 5.6 TB/s
+// -- the ten rounds of 64-bit products hiding behind it; else by the launch (129 x 4099
+// 2.9 us of the kernel's, 6.1 with its call).
 #include "lora_device.hpp"
 #include "lora_philox.hpp"
 #include "lora_train.hpp"
 
 namespace lora {
 
-template <bool F32>
-__device__ __forceinline__ float load_elem(const void* p, int64_t i) {
-  if constexpr (F32) return static_cast<const float*>(p)[i];
-  else return bf16_to_f32(static_cast<const u16*>(p)[i]);
-}
-
 // X, residual and Y may be the same tensor: a thread has read its elements before it
 // writes them.
-template <bool F32, bool RES>
-__global__ __launch_bounds__(256) void lora_dropout_kernel(const void* X, const void* R, void* Y, int64_t count,
-                                                           uint64_t seed, uint64_t offset, uint32_t thr, float scale) {
+template <bool RES>
+__global__ __launch_bounds__(256) void lora_dropout_kernel(const u16* X, const u16* R, u16* Y, int64_t count, uint64_t seed,
+                                                           uint64_t offset, uint32_t thr, float scale) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, e0 = 16 * t;
   if (e0 >= count) return;
-  constexpr int W = F32 ? 4 : 2;   // 16-byte loads of 16 elements
-  int4v x[W], r[W];
+  int4v x[2], r[2];
   const bool whole = e0 + 16 <= count;
   if (whole) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      x[i] = static_cast<const int4v*>(X)[W * t + i];
-      if constexpr (RES) r[i] = static_cast<const int4v*>(R)[W * t + i];
+    for (int i = 0; i < 2; ++i) {
+      x[i] = reinterpret_cast<const int4v*>(X)[2 * t + i];
+      if constexpr (RES) r[i] = reinterpret_cast<const int4v*>(R)[2 * t + i];
     }
   }
   uint64_t c[4] = {0ull, 0ull, 0ull, 0ull};
@@ -43,43 +42,80 @@ __global__ __launch_bounds__(256) void lora_dropout_kernel(const void* X, const 
   };
   if (whole) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
+    for (int i = 0; i < 2; ++i) {
       int4v o;
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        if constexpr (F32) {
-          o[h] = __builtin_bit_cast(int, value(4 * i + h, __builtin_bit_cast(float, (int)x[i][h]),
-                                               RES ? __builtin_bit_cast(float, (int)r[i][h]) : 0.0f));
-        } else {
-          const uint32_t xw = (uint32_t)x[i][h], rw = RES ? (uint32_t)r[i][h] : 0u;
-          const float lo = value(8 * i + 2 * h, bf16_to_f32((u16)xw), bf16_to_f32((u16)rw));
-          const float hi = value(8 * i + 2 * h + 1, bf16_to_f32((u16)(xw >> 16)), bf16_to_f32((u16)(rw >> 16)));
-          o[h] = (int)((uint32_t)f32_to_bf16(lo) | ((uint32_t)f32_to_bf16(hi) << 16));
-        }
+        const uint32_t xw = (uint32_t)x[i][h], rw = RES ? (uint32_t)r[i][h] : 0u;
+        const float lo = value(8 * i + 2 * h, bf16_to_f32((u16)xw), bf16_to_f32((u16)rw));
+        const float hi = value(8 * i + 2 * h + 1, bf16_to_f32((u16)(xw >> 16)), bf16_to_f32((u16)(rw >> 16)));
+        o[h] = (int)((uint32_t)f32_to_bf16(lo) | ((uint32_t)f32_to_bf16(hi) << 16));
       }
-      static_cast<int4v*>(Y)[W * t + i] = o;
+      reinterpret_cast<int4v*>(Y)[2 * t + i] = o;
     }
   } else {
-    for (int e = 0; e0 + e < count; ++e) {
-      const uint32_t draw = (uint32_t)((e < 8 ? (e < 4 ? c[0] : c[1]) : (e < 12 ? c[2] : c[3])) >> (16 * (e & 3))) & 0xFFFFu;
-      float y = draw < thr ? load_elem<F32>(X, e0 + e) * scale : 0.0f;
-      if constexpr (RES) y += load_elem<F32>(R, e0 + e);
-      if constexpr (F32) static_cast<float*>(Y)[e0 + e] = y;
-      else static_cast<u16*>(Y)[e0 + e] = f32_to_bf16(y);
+#pragma unroll
+    for (int e = 0; e < 15; ++e) {
+      if (e0 + e >= count) break;
+      Y[e0 + e] = f32_to_bf16(value(e, bf16_to_f32(X[e0 + e]), RES ? bf16_to_f32(R[e0 + e]) : 0.0f));
     }
   }
 }
 
-template <bool F32, bool RES>
-static hipError_t run_dropout(const DropoutArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((lora_dropout_kernel<F32, RES>), dim3((unsigned)cdiv(cdiv(a.count, 16), 256)), dim3(256), 0, st, a.X,
-                     a.residual, a.Y, a.count, a.seed, a.offset, a.thr, a.scale);
-  return hipGetLastError();
+// fp32, four draws a word of a block: word w of the wave's 256 is its 16-byte piece w's.
+template <bool RES>
+__global__ __launch_bounds__(256) void lora_dropout_f32_kernel(const float* X, const float* R, float* Y, int64_t count,
+                                                               uint64_t seed, uint64_t offset, uint32_t thr, float scale) {
+  __shared__ __attribute__((aligned(16))) uint64_t lds[4][256];
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+  const int64_t first = (int64_t)blockIdx.x * 4096 + wave * 1024, left = count - first;   // the wave's elements
+  const float *x = X + first, *r = RES ? R + first : nullptr;
+  float* y = Y + first;
+  const bool whole = left >= 1024;   // of all but the tensor's last wave
+  floatx4 xv[4], rv[4];
+  if (whole) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      xv[j] = reinterpret_cast<const floatx4*>(x)[64 * j + lane];
+      if constexpr (RES) rv[j] = reinterpret_cast<const floatx4*>(r)[64 * j + lane];
+    }
+  }
+  uint64_t c[4] = {0ull, 0ull, 0ull, 0ull};
+  if (thr < 65536u) philox_block(seed, offset, (uint64_t)blockIdx.x * 256 + threadIdx.x, c);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) lds[wave][4 * lane + i] = c[i];
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");   // the wave's own, in order
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c[j] = lds[wave][64 * j + lane];
+  auto value = [&](int e, float xe, float re) LORA_INLINE {
+    const float v = philox_draw(c, e) < thr ? xe * scale : 0.0f;
+    return RES ? v + re : v;
+  };
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    floatx4 o;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const int e = 256 * j + 4 * lane + h;
+      if (whole) o[h] = value(4 * j + h, xv[j][h], RES ? rv[j][h] : 0.0f);
+      else if (e < left) y[e] = value(4 * j + h, x[e], RES ? r[e] : 0.0f);
+    }
+    if (whole) reinterpret_cast<floatx4*>(y)[64 * j + lane] = o;
+  }
 }
 
 hipError_t launch_dropout(const DropoutArgs& a, hipStream_t st) {
-  if (a.f32) return a.residual ? run_dropout<true, true>(a, st) : run_dropout<true, false>(a, st);
-  return a.residual ? run_dropout<false, true>(a, st) : run_dropout<false, false>(a, st);
+  const dim3 grid((unsigned)cdiv(cdiv(a.count, 16), 256));
+  auto run = [&](auto kernel, auto type) {
+    using T = decltype(type);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, static_cast<const T*>(a.X), static_cast<const T*>(a.residual),
+                       static_cast<T*>(a.Y), a.count, a.seed, a.offset, a.thr, a.scale);
+    return hipGetLastError();
+  };
+  if (a.f32) return a.residual ? run(lora_dropout_f32_kernel<true>, float{}) : run(lora_dropout_f32_kernel<false>, float{});
+  return a.residual ? run(lora_dropout_kernel<true>, u16{}) : run(lora_dropout_kernel<false>, u16{});
 }
 
 }  // namespace lora
