@@ -8,7 +8,7 @@
 // A thread draws a block.  bf16: it takes the block's 32 bytes.  fp32: its 64 bytes
 // would leave lanes' loads 64 bytes apart; through LDS each lane gets the draws of four
 // 16-byte pieces instead, a load of the wave's being one run of 1 KiB (8192 x 4096: 60.8
-// -> 46.7 us, with a residual 82 -> 71; for bf16 the detour costs: 25.4 and 26.8).  Bounded by
+// -> 46.7 us, with a residual 82 -> 71; bf16 gained nothing from it).  Bounded by
 // memory where there is much of it -- 8192 x 4096 bf16 with a residual 35.8 us, 5.6 TB/s
 // -- the ten rounds of 64-bit products hiding behind it; else by the launch (129 x 4099
 // 2.9 us of the kernel's, 6.1 with its call).
@@ -54,10 +54,11 @@ __global__ __launch_bounds__(256) void lora_dropout_kernel(const u16* X, const u
       reinterpret_cast<int4v*>(Y)[2 * t + i] = o;
     }
   } else {
-#pragma unroll
-    for (int e = 0; e < 15; ++e) {
-      if (e0 + e >= count) break;
-      Y[e0 + e] = f32_to_bf16(value(e, bf16_to_f32(X[e0 + e]), RES ? bf16_to_f32(R[e0 + e]) : 0.0f));
+    for (int e = 0; e0 + e < count; ++e) {
+      const uint32_t draw = (uint32_t)((e < 8 ? (e < 4 ? c[0] : c[1]) : (e < 12 ? c[2] : c[3])) >> (16 * (e & 3))) & 0xFFFFu;
+      float y = draw < thr ? bf16_to_f32(X[e0 + e]) * scale : 0.0f;
+      if constexpr (RES) y += bf16_to_f32(R[e0 + e]);
+      Y[e0 + e] = f32_to_bf16(y);
     }
   }
 }

@@ -55,7 +55,10 @@ __device__ __forceinline__ int fp8_row_scale_at(int row, int block, int cells) {
 
 // Activations: 16 lanes a row's block, 8 columns each; a thread takes rows 16 apart,
 // whose scales are a word.  A workgroup: four blocks of the rows of a quarter cell
-// (its rows 4 q .. 4 q + 3, and those 16, 32 and 48 after them).
+// (its rows 4 q .. 4 q + 3, and those 16, 32 and 48 after them).  Bounded by memory: a
+// value is read once, held in registers while the block's largest is found by four
+// exchanges between lanes, and its byte written; 4096 x 4096 9.6 us (5.2 TB/s), 16384 x
+// 4096 36 us (5.6 TB/s), 32 x 4096 2.8 us, what a launch of a few waves takes.
 __global__ __launch_bounds__(256) void lora_fp8_quantize_rows_kernel(const u16* __restrict__ X,
                                                                      uint8_t* __restrict__ codes,
                                                                      uint8_t* __restrict__ scales, int rows, int k,
@@ -81,7 +84,9 @@ __global__ __launch_bounds__(256) void lora_fp8_quantize_rows_kernel(const u16* 
   if (lane16 == 0) *reinterpret_cast<uint32_t*>(scales + fp8_row_scale_at(cell * 64 + r16, b, cells)) = word;
 }
 
-// A weight: a workgroup a block of 128 x 128.
+// A weight: a workgroup a block of 128 x 128, all 64 values of a thread in registers, so
+// that the block's largest and its codes take one read.  11008 x 4096 21.3 us (6.3
+// TB/s).
 __global__ __launch_bounds__(256) void lora_fp8_quantize_block_kernel(const u16* __restrict__ X,
                                                                       uint8_t* __restrict__ codes,
                                                                       uint8_t* __restrict__ scales, int rows, int k,
@@ -111,7 +116,9 @@ __global__ __launch_bounds__(256) void lora_fp8_quantize_block_kernel(const u16*
   }
 }
 
-// The values of codes and scales: a lane takes 8 columns.
+// The values of codes and scales: a lane takes 8 columns.  The product with a power of
+// two and the result's bf16 are exact (4 significant bits).  11008 x 4096 21.5 us (6.3
+// TB/s).
 template <bool ROWS>
 __global__ __launch_bounds__(256) void lora_fp8_dequantize_kernel(const uint8_t* __restrict__ codes,
                                                                   const uint8_t* __restrict__ scales,
@@ -146,7 +153,10 @@ struct Fp8Product {
 // Few tokens: a workgroup forms 16 FG features x 16 TG tokens with its eight waves on
 // different stages, straight from memory without a barrier until the waves' sums are
 // added, in wave order, through LDS.  A lane loads the two 16-byte chunks of codes
-// that it multiplies; each wave has D stages' loads under way.
+// that it multiplies; each wave has D stages' loads under way.  Bounded by W's bytes:
+// 16 x 4096 x 4096 10.6 us a call with the quantisation of X (17 MB, 3.3 us at a copy's
+// rate; two launches alone 5 to 6), 32 x 11008 x 4096 16.2 us (45 MB, 8.9).  From about 32 tokens on tiles in LDS, which
+// read a token's codes once and not once per group of features, take less.
 template <int TG, int FG, int D>
 __global__ __launch_bounds__(512) void lora_fp8_few_kernel(Fp8Product p) {
   constexpr int NW = 8, FR = TG * FG;
@@ -225,7 +235,10 @@ __global__ __launch_bounds__(512) void lora_fp8_few_kernel(Fp8Product p) {
 // Very few values of X: one launch.  Every workgroup quantises X into LDS; its first
 // loads of W are under way meanwhile.  A group of 16 features is formed by KS waves
 // that share its stages, D stages' loads of W ahead; their sums are added in wave
-// order.
+// order.  X (at most 64 KiB of bf16, in L2) is quantised again by each workgroup, which
+// takes less than the launch that would do it once (2.8 us by itself): 1 x 4096 x 4096 5.0
+// us (3.4 TB/s of W; its start and its end, where few loads are under way, are the rest),
+// 1 x 32000 x 4096 20 us (6.5 TB/s).
 template <int KS, int D>
 __global__ __launch_bounds__(512) void lora_fp8_token_kernel(Fp8Product p, const u16* __restrict__ X) {
   constexpr int NW = 8;
@@ -304,6 +317,14 @@ __global__ __launch_bounds__(512) void lora_fp8_token_kernel(Fp8Product p, const
   if (c < m && col < p.n) *reinterpret_cast<uint2*>(p.out + (size_t)c * p.n + col) = bf16x4(acc);
 }
 
+// A tile of Y.  Bounded by the matrix cores where tiles of 256 x 256 fill the card: 4096 x
+// 11008 x 4096 147 to 150 us (2.5 PFLOP/s; the matrix cores multiply in 71% of the busy
+// compute units' cycles, and 688 tiles are 2.7 rounds of 256, 3 in time); below that by
+// how copies into LDS, reads from it and products overlap within one workgroup, about 0.6
+// us each of a 256 x 128 tile's stage of 0.6 (few workgroups) to 0.9 us: 1531 x 4104 x
+// 3208 24.4 us.  LDS has no conflicts to speak of (3% of its cycles); XCD-aware tile order
+// (tile_coords): the 256 x 256 example reads 312 MB from memory and its last-level cache,
+// 62 without any repetition.
 template <class Core, int BM, int BN, int NT>
 __global__ __launch_bounds__(NT) void lora_fp8_fwd_kernel(Fp8Product p) {
   __shared__ __attribute__((aligned(1024))) char smem[Core::SMEM];
@@ -320,6 +341,9 @@ __global__ __launch_bounds__(NT) void lora_fp8_fwd_kernel(Fp8Product p) {
   store_tile<Core, BM, BN, NT>(acc, smem, p.out + (size_t)m0 * p.n + n0, (size_t)p.n, p.m - m0, p.n - n0);
 }
 
+// A tile of dX, or of its sum over a part of n.  W stands as the forward reads it (its rows
+// along k), so LDS reads turn it.  1024 x 4096 x 11008 47 to 49 us (172 tiles of 256 x 256
+// on 256 compute units; 68% of the busy ones' cycles multiply), 2048 x 4096 x 4096 34.5 us.
 template <class Core, int BM, int NT>
 __global__ __launch_bounds__(NT) void lora_fp8_bwd_kernel(Fp8Product p) {
   __shared__ __attribute__((aligned(1024))) char smem[Core::SMEM];
@@ -349,7 +373,8 @@ __global__ __launch_bounds__(NT) void lora_fp8_bwd_kernel(Fp8Product p) {
   }
 }
 
-// The sum of a split product's parts, in their order: 4 columns a thread.
+// The sum of a split product's parts, in their order (the result does not depend on who
+// comes first): 4 columns a thread, from the last-level cache where the parts still are.
 __global__ __launch_bounds__(256) void lora_fp8_join_kernel(const float* __restrict__ sums, u16* __restrict__ out, int m,
                                                             int k, int tiles_n, int tiles, int splits) {
   const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
