@@ -542,7 +542,7 @@ lora_status lora_linear_fp8_bwd(const lora_bf16* dY, const uint8_t* W_codes, con
  *   X, residual, Y  [count] of type `dtype` (another: LORA_ERR_UNSUPPORTED), 16-byte
  *             aligned; residual may be NULL (none).  Y may be X or the residual
  *             itself; any other overlap is LORA_ERR_ALIAS
- *   count     1 .. 2^40
+ *   count     1 .. 2^35 (less: LORA_ERR_SHAPE, more: LORA_ERR_UNSUPPORTED)
  *   p         dropout rate, 0 <= p < 1 (else LORA_ERR_SHAPE)
  * Computed in fp32 and rounded once.  What X holds in a dropped place, NaN and
  * infinities included, does not matter.
@@ -563,8 +563,8 @@ lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtyp
  *   labels    [rows].  A label outside [0, vocab) is none: the row's loss is 0 and it
  *             has no part in the gradients, whatever its X holds
  *   loss      [rows] fp32, written
- *   saved     [rows, 2] fp32: written by the forward for the backward (there may be
- *             NULL)
+ *   saved     [rows, 2] fp32: written by the forward for the backward (NULL in the
+ *             forward: not wanted)
  *   dloss     [rows] fp32, read only
  *   dX, dW    [rows, k], [vocab, k] bf16, written; one of them may be NULL
  *   workspace at least lora_linear_xent_workspace_size(rows, vocab, k, dx, dw) bytes
@@ -572,8 +572,9 @@ lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtyp
  *             for the forward; a call with fewer outputs needs no more), 16-byte
  *             aligned, not used concurrently
  * Logits, their exponentials and all sums are fp32; G enters its products as bf16.
- * A row of labels with a NaN or an infinity among its logits has loss and gradients
- * NaN.  rows >= 1, vocab >= 1, k >= 8 and a multiple of 8 (LORA_ERR_SHAPE), rows and
+ * A row with a label and a NaN or plus infinity among its logits has loss and dX NaN,
+ * and so has dW; minus infinity is a logit of probability 0 (of the label: an infinite
+ * loss), whose entry of dX is 0 times a W that is not finite.  rows >= 1, vocab >= 1, k >= 8 and a multiple of 8 (LORA_ERR_SHAPE), rows and
  * vocab at most 2^20, k at most 2^16, rows k at most 2^30 (LORA_ERR_UNSUPPORTED).
  *
  * lora_linear_xent_step: loss and gradients in one call, for a dloss known

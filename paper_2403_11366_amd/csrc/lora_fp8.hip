@@ -117,7 +117,7 @@ __global__ __launch_bounds__(256) void lora_fp8_quantize_block_kernel(const u16*
 }
 
 // The values of codes and scales: a lane takes 8 columns.  The product with a power of
-// two and the result's bf16 are exact (4 significant bits).  11008 x 4096 21.5 us (6.3
+// two and the result's bf16 are exact from 2^-126 on (4 significant bits).  11008 x 4096 21.5 us (6.3
 // TB/s).
 template <bool ROWS>
 __global__ __launch_bounds__(256) void lora_fp8_dequantize_kernel(const uint8_t* __restrict__ codes,
@@ -155,8 +155,9 @@ struct Fp8Product {
 // added, in wave order, through LDS.  A lane loads the two 16-byte chunks of codes
 // that it multiplies; each wave has D stages' loads under way.  Bounded by W's bytes:
 // 16 x 4096 x 4096 10.6 us a call with the quantisation of X (17 MB, 3.3 us at a copy's
-// rate; two launches alone 5 to 6), 32 x 11008 x 4096 16.2 us (45 MB, 8.9).  From about 32 tokens on tiles in LDS, which
-// read a token's codes once and not once per group of features, take less.
+// rate; two launches alone 5 to 6), 32 x 11008 x 4096 16.2 us (45 MB, 8.9).
+// From about 32 tokens on tiles in LDS, which read a token's codes once and not once per
+// group of features, take less.
 template <int TG, int FG, int D>
 __global__ __launch_bounds__(512) void lora_fp8_few_kernel(Fp8Product p) {
   constexpr int NW = 8, FR = TG * FG;

@@ -16,7 +16,7 @@ constexpr int64_t kMaxElems = int64_t(1) << 30;     // any one matrix of theirs,
 constexpr int64_t kMaxRows = int64_t(1) << 20;      // rows of the loss
 constexpr int64_t kMaxVocab = int64_t(1) << 20;     // columns of its logits
 constexpr int64_t kMaxHidden = int64_t(1) << 16;    // width of its rows
-constexpr int64_t kMaxCount = int64_t(1) << 40;     // elements of a dropout call
+constexpr int64_t kMaxCount = int64_t(1) << 35;     // elements of a dropout call: a thread per 16, fewer than 2^32 of them
 
 struct Range {
   uintptr_t lo, hi;  // [lo, hi)

@@ -598,7 +598,12 @@ struct XentCall {
     return hipGetLastError();
   }
   hipError_t forward(float* saved) const {
-    LORA_TRY(run_logits<XENT_STATS>(p, logits(), st));
+    XentLogits q = logits();
+    const int most = (1 << 22) / p.tiles_m;   // (a launch has fewer than 2^32 threads; tiles_m is at most 2^14)
+    for (q.tile0 = 0; q.tile0 < p.vtiles; q.tile0 += most) {
+      q.tiles_n = std::min(most, p.vtiles - q.tile0);
+      LORA_TRY(run_logits<XENT_STATS>(p, q, st));
+    }
     return rows(saved, nullptr, nullptr);
   }
   hipError_t backward(const float* saved) const {

@@ -175,6 +175,55 @@ def test_not_a_number(rows):
         assert all(np.array_equal(a, b) for a, b in zip(got, want)), how
 
 
+@pytest.mark.parametrize("rows,vocab", [(6, 1000), (300, 1300)])
+def test_logits_of_minus_infinity(rows, vocab):
+    """They have probability 0; a row with such a label has an infinite loss."""
+    k = 64
+    x, w, labels, d = case(rows, vocab, k, 12, sure=0.0)
+    x = f64(x)
+    x[:, 0] = np.abs(x[:, 0]) + 0.125
+    x, labels = to_bits(x), np.where(labels < vocab, labels, -1)
+    w[7, 0] = w[vocab - 1, 0] = 0xFF80
+    labels[2], labels[4] = 7, vocab - 1
+    labels = np.where((np.arange(rows) == 2) | (np.arange(rows) == 4), labels, np.where(labels % vocab == 7, 8, labels)).astype(np.int32)
+    labels = np.where((np.arange(rows) != 4) & (labels == vocab - 1), 8, labels).astype(np.int32)
+    kept = [v for v in range(vocab) if v not in (7, vocab - 1)]
+    at = {v: i for i, v in enumerate(kept)}
+    rest = np.array([at.get(y, -1) for y in labels], np.int32)
+    want, tol = bounds(f64(x), f64(w[kept]), rest, d.astype(np.float64))
+    for how in ("step", "two"):
+        loss, dX, dW = run(x, w, labels, d, how, True, how == "two")
+        assert (loss[[2, 4]] == np.inf).all(), how
+        some = np.ones(rows, bool)
+        some[[2, 4]] = False
+        assert (np.abs(loss - want[0])[some] <= tol[0][some]).all(), how
+        # where W is finite, the gradient of those rows is the one without such columns
+        assert (np.abs(dX - want[1])[some][:, 1:] <= tol[1][some][:, 1:]).all(), how
+
+
+def test_more_tiles_than_a_launch_has():
+    """2^20 rows and 2^19 columns: a thread for each 128 logits would be 2^32 of them.  The
+    loss of some rows against the definition."""
+    import torch
+    import paper_2403_11366_amd as lora
+    rows, vocab, k = 1 << 20, 1 << 19, 8
+    g = torch.Generator("cuda").manual_seed(3)
+    X = torch.randn(rows, k, device="cuda", generator=g).bfloat16()
+    W = torch.randn(vocab, k, device="cuda", generator=g).bfloat16()
+    labels = torch.randint(0, vocab, (rows,), device="cuda", dtype=torch.int32, generator=g)
+    loss = torch.empty(rows, device="cuda")
+    ws = torch.empty(lora.lora_linear_xent_workspace_size(rows, vocab, k), dtype=torch.uint8, device="cuda")
+    lora.lora_linear_xent_fwd(X, W, labels, loss, None, ws)
+    torch.cuda.synchronize()
+    at = [0, 1, 255, 256, 77777, rows // 2 - 1, rows // 2, rows - 257, rows - 1]
+    x, w, y, got = X[at].double().cpu(), W.double().cpu(), labels[at].long().cpu(), loss[at].double().cpu()
+    z = x @ w.t()
+    want = torch.logsumexp(z, 1) - z.gather(1, y[:, None])[:, 0]
+    size = (x.abs() @ w.abs().t()).max()   # as above, |z| and the reference at most size log2 e, 2^12 tiles
+    tol = 2 * (9 * 2.0 ** -24 * size + 2.0 ** -23 * (1.5 * 2 * 1.45 * size + 66)) + (64 + 4096) * 2.0 ** -24
+    assert ((got - want).abs() <= tol + 2.0 ** -24 * want).all()
+
+
 def test_no_labels_at_all():
     x, w, labels, d = case(150, 500, 64, 2)
     labels[:] = -100
