@@ -236,7 +236,7 @@ __global__ __launch_bounds__(512) void lora_fp8_few_kernel(Fp8Product p) {
 // Very few values of X: one launch.  Every workgroup quantises X into LDS; its first
 // loads of W are under way meanwhile.  A group of 16 features is formed by KS waves
 // that share its stages, D stages' loads of W ahead; their sums are added in wave
-// order.  X (at most 64 KiB of bf16, in L2) is quantised again by each workgroup, which
+// order.  X (at most 32 KiB, in L2) is quantised again by each workgroup, which
 // takes less than the launch that would do it once (2.8 us by itself): 1 x 4096 x 4096 5.0
 // us (3.4 TB/s of W; its start and its end, where few loads are under way, are the rest),
 // 1 x 32000 x 4096 20 us (6.5 TB/s).
@@ -318,7 +318,20 @@ __global__ __launch_bounds__(512) void lora_fp8_token_kernel(Fp8Product p, const
   if (c < m && col < p.n) *reinterpret_cast<uint2*>(p.out + (size_t)c * p.n + col) = bf16x4(acc);
 }
 
-// A tile of Y.  Bounded by the matrix cores where tiles of 256 x 256 fill the card: 4096 x
+// A tile's part of a split product: its rows of BN sums, [split][tile][row][column].
+template <class Core, int BN>
+__device__ __forceinline__ void store_sums(const typename Core::Acc& acc, float* to) {
+  constexpr int FA = std::extent_v<typename Core::Acc, 0>, FB = std::extent_v<typename Core::Acc, 1>;
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+#pragma unroll
+  for (int b = 0; b < FB; ++b)
+#pragma unroll
+    for (int a = 0; a < FA; ++a)
+      *reinterpret_cast<floatx4*>(to + (Core::row0(wave) + 16 * b + (lane & 15)) * BN + Core::col(wave, a) +
+                                  4 * (lane >> 4)) = acc[a][b];
+}
+
+// A tile of Y, or of its sum over a part of k.  Bounded by the matrix cores where tiles of 256 x 256 fill the card: 4096 x
 // 11008 x 4096 147 to 150 us (2.5 PFLOP/s; the matrix cores multiply in 71% of the busy
 // compute units' cycles, and 688 tiles are 2.7 rounds of 256, 3 in time); below that by
 // how copies into LDS, reads from it and products overlap within one workgroup, about 0.6
@@ -326,20 +339,29 @@ __global__ __launch_bounds__(512) void lora_fp8_token_kernel(Fp8Product p, const
 // 3208 24.4 us.  LDS has no conflicts to speak of (3% of its cycles); XCD-aware tile order
 // (tile_coords): the 256 x 256 example reads 312 MB from memory and its last-level cache,
 // 62 without any repetition.
-template <class Core, int BM, int BN, int NT>
+template <class Core, int BM, int BN, int NT, bool SPLIT>
 __global__ __launch_bounds__(NT) void lora_fp8_fwd_kernel(Fp8Product p) {
   __shared__ __attribute__((aligned(1024))) char smem[Core::SMEM];
-  int tm, tn;
-  tile_coords(p.tiles_m, p.tiles_n, 8, (int)blockIdx.x, tm, tn);
-  const int m0 = tm * BM, n0 = tn * BN, blocks = (p.k + 127) / 128;
-  const uint32_t row = (uint32_t)blocks * 128;
-  const NtTile t{make_rsrc(p.Ac + (size_t)m0 * row, (uint64_t)min(BM, p.m - m0) * row),
-                 make_rsrc(p.Wc + (size_t)n0 * row, (uint64_t)min(BN, p.n - n0) * row), row, row, row, blocks};
-  const int nb = (p.n + 127) / 128;
-  const Scales sc{p.As, p.Ws, (p.m + 63) / 64, nb * blocks, n0 / 128 * blocks, 1, blocks, nb - n0 / 128};
+  int tm, tn, split = 0;
+  if constexpr (SPLIT) split = (int)blockIdx.x / (p.tiles_m * p.tiles_n);
+  tile_coords(p.tiles_m, p.tiles_n, 8, (int)blockIdx.x - split * p.tiles_m * p.tiles_n, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN, blocks = (p.k + 127) / 128, nb = (p.n + 127) / 128, cells = (p.m + 63) / 64;
+  int s0 = 0, s1 = blocks;   // the workgroup's stages; operands and scales begin at s0
+  if constexpr (SPLIT) {
+    s0 = (int)((int64_t)blocks * split / p.splits);
+    s1 = (int)((int64_t)blocks * (split + 1) / p.splits);
+  }
+  const uint32_t row = (uint32_t)blocks * 128, skip = (uint32_t)s0 * 128;
+  const NtTile t{make_rsrc(p.Ac + (size_t)m0 * row + skip, (uint64_t)min(BM, p.m - m0) * row - skip),
+                 make_rsrc(p.Wc + (size_t)n0 * row + skip, (uint64_t)min(BN, p.n - n0) * row - skip), row, row,
+                 row - skip, s1 - s0};
+  const Scales sc{p.As + (size_t)s0 * cells * 64, p.Ws, cells, nb * blocks, n0 / 128 * blocks + s0, 1, blocks, nb - n0 / 128};
   typename Core::Acc acc;
   Core::run(t, sc, m0, smem, acc);
-  store_tile<Core, BM, BN, NT>(acc, smem, p.out + (size_t)m0 * p.n + n0, (size_t)p.n, p.m - m0, p.n - n0);
+  if constexpr (SPLIT)
+    store_sums<Core, BN>(acc, p.sums + ((size_t)split * p.tiles_m * p.tiles_n + (size_t)tm * p.tiles_n + tn) * BM * BN);
+  else
+    store_tile<Core, BM, BN, NT>(acc, smem, p.out + (size_t)m0 * p.n + n0, (size_t)p.n, p.m - m0, p.n - n0);
 }
 
 // A tile of dX, or of its sum over a part of n.  W stands as the forward reads it (its rows
@@ -361,31 +383,25 @@ __global__ __launch_bounds__(NT) void lora_fp8_bwd_kernel(Fp8Product p) {
   Core::run(t, sc, m0, s0, s1, smem, acc);
   if (p.splits == 1) {
     store_tile<Core, BM, 256, NT>(acc, smem, p.out + (size_t)m0 * p.k + l0, (size_t)p.k, p.m - m0, p.k - l0);
-  } else {   // [split][tile][row][column]
-    float* to = p.sums + ((size_t)split * tiles + (size_t)tm * p.tiles_n + tn) * BM * 256;
-    constexpr int FA = std::extent_v<typename Core::Acc, 0>, FB = std::extent_v<typename Core::Acc, 1>;
-    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-#pragma unroll
-    for (int b = 0; b < FB; ++b)
-#pragma unroll
-      for (int a = 0; a < FA; ++a)
-        *reinterpret_cast<floatx4*>(to + (Core::row0(wave) + 16 * b + (lane & 15)) * 256 + Core::col(wave, a) +
-                                    4 * (lane >> 4)) = acc[a][b];
+  } else {
+    store_sums<Core, 256>(acc, p.sums + ((size_t)split * tiles + (size_t)tm * p.tiles_n + tn) * BM * 256);
   }
 }
 
 // The sum of a split product's parts, in their order (the result does not depend on who
 // comes first): 4 columns a thread, from the last-level cache where the parts still are.
+// Tiles of 64 x BN; out has m rows of n.
+template <int BN>
 __global__ __launch_bounds__(256) void lora_fp8_join_kernel(const float* __restrict__ sums, u16* __restrict__ out, int m,
-                                                            int k, int tiles_n, int tiles, int splits) {
+                                                            int n, int tiles_n, int tiles, int splits) {
   const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int per = k / 4, row = (int)(e / per), col = 4 * (int)(e - (int64_t)row * per);
+  const int per = n / 4, row = (int)(e / per), col = 4 * (int)(e - (int64_t)row * per);
   if (row >= m) return;
-  const float* from = sums + ((size_t)(row / 64) * tiles_n + col / 256) * 64 * 256 + (row & 63) * 256 + (col & 255);
+  const float* from = sums + ((size_t)(row / 64) * tiles_n + col / BN) * 64 * BN + (row & 63) * BN + col % BN;
   floatx4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const floatx4*>(from + (size_t)s * tiles * 64 * 256);
-  *reinterpret_cast<uint2*>(out + (size_t)row * k + col) = bf16x4(v);
+  for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const floatx4*>(from + (size_t)s * tiles * 64 * BN);
+  *reinterpret_cast<uint2*>(out + (size_t)row * n + col) = bf16x4(v);
 }
 
 hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, hipStream_t st) {
@@ -422,7 +438,13 @@ static Fp8Product product_of(const Fp8Args& a, const Fp8Layout& L, const Fp8Plan
 
 template <class Core, int BM, int BN, int NT>
 static hipError_t run_fwd_tile(const Fp8Plan& p, const Fp8Product& q, hipStream_t st) {
-  hipLaunchKernelGGL((lora_fp8_fwd_kernel<Core, BM, BN, NT>), dim3((unsigned)p.grid), dim3(NT), 0, st, q);
+  hipLaunchKernelGGL((lora_fp8_fwd_kernel<Core, BM, BN, NT, false>), dim3((unsigned)p.grid), dim3(NT), 0, st, q);
+  return hipGetLastError();
+}
+template <int BN>
+static hipError_t run_join(const Fp8Plan& p, const Fp8Product& q, int cols, hipStream_t st) {
+  hipLaunchKernelGGL((lora_fp8_join_kernel<BN>), dim3((unsigned)cdiv((int64_t)q.m * (cols / 4), 256)), dim3(256), 0, st, q.sums,
+                     q.out, q.m, cols, p.tiles_n, p.tiles_m * p.tiles_n, p.splits);
   return hipGetLastError();
 }
 template <int TG, int D>
@@ -449,6 +471,13 @@ hipError_t launch_fp8_fwd(const Fp8Args& a, hipStream_t st) {
     case FP8_FEW_2: return run_few<2, 2>(p, q, st);
     case FP8_64x64: return run_fwd_tile<NtCore<Fp8, 64, 64, 1, 4, 4, false>, 64, 64, 256>(p, q, st);
     case FP8_64x128: return run_fwd_tile<NtCore<Fp8, 64, 128, 1, 4, 3, false>, 64, 128, 256>(p, q, st);
+    case FP8_64x128_DEEP: {
+      using Core = NtCore<Fp8, 64, 128, 1, 4, 4, false>;
+      if (p.splits == 1) return run_fwd_tile<Core, 64, 128, 256>(p, q, st);
+      hipLaunchKernelGGL((lora_fp8_fwd_kernel<Core, 64, 128, 256, true>), dim3((unsigned)p.grid), dim3(256), 0, st, q);
+      const hipError_t f = hipGetLastError();
+      return f == hipSuccess ? run_join<128>(p, q, (int)a.n, st) : f;
+    }
     case FP8_128x128: return run_fwd_tile<NtCore<Fp8, 128, 128, 2, 4, 3, false>, 128, 128, 512>(p, q, st);
     case FP8_256x128: return run_fwd_tile<NtCore<Fp8, 256, 128, 4, 2, 3, false>, 256, 128, 512>(p, q, st);
     default: return run_fwd_tile<NtBig<Fp8, false>, 256, 256, 512>(p, q, st);
@@ -472,10 +501,7 @@ hipError_t launch_fp8_bwd(const Fp8Args& a, hipStream_t st) {
     case FP8_BACK_128x256: e = run_bwd_tile<NnCore<Fp8, 128, 256, 2, 4, 3>, 128, 512>(p, q, st); break;
     default: e = run_bwd_tile<NnBig<Fp8>, 256, 512>(p, q, st); break;
   }
-  if (e != hipSuccess || p.splits == 1) return e;
-  hipLaunchKernelGGL(lora_fp8_join_kernel, dim3((unsigned)cdiv(a.m * (a.k / 4), 256)), dim3(256), 0, st, q.sums, a.out,
-                     (int)a.m, (int)a.k, p.tiles_n, p.tiles_m * p.tiles_n, p.splits);
-  return hipGetLastError();
+  return e != hipSuccess || p.splits == 1 ? e : run_join<256>(p, q, (int)a.k, st);
 }
 
 }  // namespace lora

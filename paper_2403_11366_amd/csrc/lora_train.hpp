@@ -60,8 +60,8 @@ struct Fp8Args {
 // Kernels of the forward: one launch that quantises X on its way for very few values
 // of it; else X is quantised before, and the product is formed by waves on different
 // stages straight from memory (few tokens) or by tiles staged in LDS.  The backward
-// has tiles alone, whose contraction workgroups may share.
-enum Fp8Kind { FP8_TOKEN_8, FP8_TOKEN_2, FP8_FEW_1, FP8_FEW_2, FP8_64x64, FP8_64x128, FP8_128x128, FP8_256x128, FP8_256x256 };
+// has tiles alone.  Workgroups may share the contractions of tiles of 64 rows.
+enum Fp8Kind { FP8_TOKEN_8, FP8_TOKEN_2, FP8_FEW_1, FP8_FEW_2, FP8_64x64, FP8_64x128, FP8_64x128_DEEP, FP8_128x128, FP8_256x128, FP8_256x256 };
 enum Fp8BackKind { FP8_BACK_64x256, FP8_BACK_128x256, FP8_BACK_256x256 };
 
 struct Fp8Plan {
@@ -75,20 +75,27 @@ struct Fp8Plan {
 // Tiles are chosen by their estimated time in us, launches and the quantisation left
 // out: a round of workgroups that fills the compute units takes c + full x stages, one
 // of few of them c + light x stages, the last one in between.
-//   Forward, fitted to k = 2048 to 11008 (us): 64 x 4096 x 4096 9.9 on 64 x 64 (14.6 on
-// 64 x 128, 15.0 from memory), 24 x 32000 x 4096 21.8 on both, 128 x 11008 x 4096 18.1
-// on 64 x 128 (21 on 64 x 64, 22 on 128 x 128), 1024 x 4096 x 4096 22.4 on 128 x 128 (28
+//   Forward, fitted to k = 2048 to 11008 (us): 64 x 4096 x 4096 9.3 on 64 x 64 (13 on 64
+// x 128, 15.0 from memory), 128 x 11008 x 4096 17.3 on 64 x 128 (21 on 64 x 64, 22 on
+// 128 x 128), 1024 x 4096 x 4096 22.4 on 128 x 128 (28
 // on 64 x 128, 29 on 256 x 128), 1531 x 4104 x 3208 24.7 on 256 x 128 (33 on 128 x 128,
 // 36 on 256 x 256), 4096 x 4096 x 4096 54 on 256 x 256 (63 on 256 x 128).
 //   Backward: 200 x 4096 x 4096 23 on 64 x 256, 17 with four workgroups to a tile, 1024
 // x 4096 x 4096 27.8 on 64 x 256 (30 on 128 x 256, 43 on 256 x 256), 2048 x 4096 x 4096
 // 34.5 on 128 x 256 (53, 47), 1024 x 4096 x 11008 47 on 256 x 256 (60 on 128 x 256).
+//   64 x 128 has four stages in LDS where its tiles are at most a compute unit's one, for
+// the latency of memory (512 x 4096 x 4096 14.9, with three 17.8), and three where there
+// are more, for two workgroups to a unit (64 x 128256 x 4096 114, with four 124).  With
+// four, workgroups may share the contractions of few tiles: with X's quantisation 64 x
+// 4096 x 11008 32.9 -> 20.1, 128 x 4096 x 11008 32.9 -> 23.8, 64 x 1024 x 8192 18.5 ->
+// 13.3.
 struct TileCost {
   int kind, bm, bn, block;
   double c, light, full;
 };
-constexpr TileCost kFp8Tiles[5] = {{FP8_64x64, 64, 64, 256, 1.5, 0.26, 0.29},
+constexpr TileCost kFp8Tiles[6] = {{FP8_64x64, 64, 64, 256, 1.5, 0.26, 0.29},
                                    {FP8_64x128, 64, 128, 256, 1.8, 0.40, 0.42},
+                                   {FP8_64x128_DEEP, 64, 128, 256, 1.8, 0.35, 0.41},
                                    {FP8_128x128, 128, 128, 512, 2.5, 0.42, 0.60},
                                    {FP8_256x128, 256, 128, 512, 4.0, 0.58, 0.90},
                                    {FP8_256x256, 256, 256, 512, 6.0, 1.03, 1.45}};
@@ -110,6 +117,10 @@ inline Fp8Plan fp8_plan_of(int kind, int64_t rows, int64_t cols, int bm, int bn,
   return p;
 }
 
+// What sharing a tile's contraction costs: the join's launch, the sums in memory.
+inline double split_time(const Fp8Plan& p, const TileCost& t) {
+  return p.splits > 1 ? 4.5 + (double)p.grid * t.bm * t.bn * 8 / 4.5e6 : 0.0;
+}
 // The one launch up to 2^14 values of X: each workgroup quantises all of them (1 x 4096
 // x 4096 6.2 us against 2.4 + 5.0 in two launches, 4 x 4096 x 4096 7.0 against 2.4 +
 // 5.5; 8 x 4096 x 4096 8.5 against 2.4 + 5.8).  Its LDS: X's codes and scales, the waves'
@@ -135,8 +146,15 @@ inline Fp8Plan plan_fp8_fwd(int64_t m, int64_t n, int64_t k) {
     }
   };
   for (const TileCost& t : kFp8Tiles) {
-    const Fp8Plan p = fp8_plan_of(t.kind, m, n, t.bm, t.bn, t.block, 1);
-    consider(p, tile_time(t, p.grid, s));
+    const int64_t tiles = cdiv(m, t.bm) * cdiv(n, t.bn);
+    if (t.kind == FP8_64x128_DEEP) {   // one workgroup to a compute unit
+      for (int64_t splits = 1; splits <= std::min<int64_t>(256 / tiles, std::max<int64_t>(1, (int64_t)s / 4)); ++splits) {
+        const Fp8Plan p = fp8_plan_of(t.kind, m, n, t.bm, t.bn, t.block, (int)splits);
+        consider(p, tile_time(t, p.grid, (double)cdiv((int64_t)s, splits)) + split_time(p, t));
+      }
+    } else {
+      consider(fp8_plan_of(t.kind, m, n, t.bm, t.bn, t.block, 1), tile_time(t, tiles, s));
+    }
   }
   if (m <= 16) {
     const Fp8Plan p = fp8_plan_of(FP8_FEW_1, m, n, 16, 16, 512, 1);
@@ -159,8 +177,7 @@ inline Fp8Plan plan_fp8_bwd(int64_t m, int64_t n, int64_t k) {
     const int64_t most = t.kind == FP8_BACK_64x256 ? std::max<int64_t>(1, std::min<int64_t>(256 / tiles, stages / 4)) : 1;
     for (int64_t splits = 1; splits <= most; ++splits) {
       const Fp8Plan p = fp8_plan_of(t.kind, m, k, t.bm, t.bn, t.block, (int)splits);
-      double time = tile_time(t, p.grid, (double)cdiv(stages, splits));
-      if (splits > 1) time += 4.5 + (double)p.grid * t.bm * t.bn * 8 / 4.5e6;
+      const double time = tile_time(t, p.grid, (double)cdiv(stages, splits)) + split_time(p, t);
       if (time < least) {
         least = time;
         best = p;
@@ -173,11 +190,12 @@ struct Fp8Layout {
   size_t codes, scales, sums, total;
 };
 inline Fp8Layout fp8_fwd_layout(int64_t m, int64_t n, int64_t k) {
-  (void)n;
   Fp8Layout L;
   L.codes = 0;
   L.scales = region(fp8_codes_bytes(m, k));
-  L.sums = L.total = L.scales + region(fp8_scales_bytes(m, k, 1));
+  L.sums = L.scales + region(fp8_scales_bytes(m, k, 1));
+  const Fp8Plan p = plan_fp8_fwd(m, n, k);
+  L.total = L.sums + (p.splits > 1 ? (size_t)p.grid * 64 * 128 * 4 : 0);
   return L;
 }
 inline Fp8Layout fp8_bwd_layout(int64_t m, int64_t n, int64_t k) {

@@ -87,10 +87,13 @@ static int plans() {
         if (f.kind <= FP8_TOKEN_2) HOLDS(m <= kFp8TokenRows && fp8_token_lds(m, k) <= 160 * 1024 && m * fp8_blocks(k) * 16 < (1 << 19), m, n, k);
         if (f.kind == FP8_FEW_1) HOLDS(m <= 16 && f.block == 512, m, n, k);
         if (f.kind == FP8_FEW_2) HOLDS(m <= 32 && f.block == 512, m, n, k);
-        HOLDS(f.splits == 1 && (b.splits == 1 || b.kind == FP8_BACK_64x256), m, n, k);   // the join's tiles have 64 rows
+        HOLDS(f.splits == 1 || f.kind == FP8_64x128_DEEP, m, n, k);   // the join's tiles have 64 rows
+        HOLDS(b.splits == 1 || b.kind == FP8_BACK_64x256, m, n, k);
+        HOLDS(f.splits <= fp8_blocks(k), m, n, k);
         HOLDS(lf.scales >= fp8_codes_bytes(m, k) && lf.sums >= lf.scales + fp8_scales_bytes(m, k, 1), m, n, k);
         HOLDS(lb.scales >= fp8_codes_bytes(m, n) && lb.sums >= lb.scales + fp8_scales_bytes(m, n, 1), m, n, k);
-        HOLDS(lf.total >= lf.sums && lb.total >= lb.sums, m, n, k);
+        HOLDS(lf.total >= lf.sums + (f.splits > 1 ? (size_t)f.grid * 64 * 128 * 4 : 0), m, n, k);
+        HOLDS(lb.total >= lb.sums + (b.splits > 1 ? (size_t)b.grid * 64 * 256 * 4 : 0), m, n, k);
         // what the tiles' 32-bit offsets reach: 256 rows of codes, a stage's scales
         HOLDS(fp8_blocks(k) * 128 * 256 < (int64_t(1) << 31) && fp8_blocks(n) * 128 * 256 < (int64_t(1) << 31), m, n, k);
         HOLDS((int64_t)fp8_scales_bytes(m, k, 1) < (int64_t(1) << 31) && (int64_t)fp8_scales_bytes(m, n, 1) < (int64_t(1) << 31), m, n, k);
@@ -139,7 +142,8 @@ int main(int argc, char** argv) {
         printf("logits%d grad%d join%d pieces%d local%d\n", p.kind, p.grad_kind, p.splits > 1 ? p.grad_kind : -1, p.pieces > 1, p.local ? p.grad_kind : -1);
         continue;
       }
-      printf("%d\n", (int)(strcmp(argv[1], "fwd") == 0 ? lora::plan_fp8_fwd(m, n, k) : lora::plan_fp8_bwd(m, n, k)).kind);
+      const lora::Fp8Plan p = strcmp(argv[1], "fwd") == 0 ? lora::plan_fp8_fwd(m, n, k) : lora::plan_fp8_bwd(m, n, k);
+      printf("%d%s\n", p.kind, p.splits > 1 ? "s" : "");
     }
     return 0;
   }

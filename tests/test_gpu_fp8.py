@@ -157,7 +157,8 @@ LINEAR = [(1, 8, 8), (1, 4096, 4096), (2, 24, 40), (3, 520, 264), (4, 1024, 2048
           (65, 72, 256), (100, 1032, 520), (128, 128, 4096), (129, 392, 768), (200, 5120, 264), (255, 264, 2056),
           (256, 256, 256), (257, 520, 512), (300, 4096, 1024), (513, 1544, 776), (700, 2048, 2048), (1000, 1000, 1000),
           (1024, 4096, 264), (1531, 4104, 1608), (2048, 4096, 512), (2050, 8200, 256), (4100, 4360, 8), (3000, 3976, 128), (1, 17000, 264), (3, 20008, 520), (30, 3000, 2056),
-          (90, 2000, 1032), (1100, 4200, 520), (1600, 1304, 392), (250, 8000, 520), (5, 4096, 4096), (12, 304, 8200)]
+          (90, 2000, 1032), (1100, 4200, 520), (1600, 1304, 392), (250, 8000, 520), (5, 4096, 4096), (12, 304, 8200),
+          (50, 33000, 136), (64, 1024, 8192), (40, 264, 11008), (200, 1000, 4104), (126, 520, 16392), (500, 4096, 264)]
 
 
 @pytest.mark.parametrize("m,n,k", LINEAR)

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PKG = os.path.join(ROOT, "paper_2403_11366_amd")
 HOST_SAN = ["-O1", "-g", "-fno-sanitize-recover=all", "-fno-omit-frame-pointer", "-std=c++17"]
 SAN = ["-Xarch_host", "-fsanitize=address,undefined"]
-KINDS = {"fwd": 9, "bwd": 3}   # kernels of the 8-bit forward and backward
+# kernels of the 8-bit forward and backward; s: with a contraction shared by workgroups
+KINDS = {"fwd": {str(i) for i in range(10)} | {"6s"}, "bwd": {"0", "0s", "1", "2"}}
 
 
 def _run(cmd, **kw):
@@ -48,7 +49,7 @@ def test_gpu_sizes_reach_every_kernel_of_the_8_bit_layer(driver, way):
     import test_gpu_fp8 as gpu
     sizes = [str(x) for m, n, k in gpu.LINEAR for x in ((m, n, k) if way == "fwd" else (m, k, n))]
     text = _run([driver, way] + sizes, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
-    assert set(text.split()) == {str(i) for i in range(KINDS[way])}
+    assert set(text.split()) == KINDS[way]
 
 
 def test_gpu_sizes_reach_every_kernel_of_the_loss(driver):
