@@ -175,6 +175,26 @@ def test_not_a_number(rows):
         assert all(np.array_equal(a, b) for a, b in zip(got, want)), how
 
 
+@pytest.mark.parametrize("rows,vocab,k,spread", [(1, 1, 8, 1.0), (1, 500, 64, 0.01), (3, 40000, 264, 0.01), (40, 700, 520, 0.01),
+                                                 (2500, 600, 72, 0.01), (5000, 30011, 40, 0.01), (300, 3000, 1032, 2.5)])
+def test_labels_rows_of_dW(rows, vocab, k, spread):
+    """A label's entry of G enters dW with more than its bf16: where all other entries are
+    small, a label's row of dW is off by its own rounding.  Some labels are many rows'."""
+    x, w, labels, d = case(rows, vocab, k, rows + vocab, spread=spread, sure=0.0)
+    labels[rows // 3:rows // 2] = vocab - 1
+    fx, fw, fd = f64(x), f64(w), d.astype(np.float64)
+    (_, _, want), (_, _, tol) = bounds(fx, fw, labels, fd)
+    got = run(x, w, labels, d, "two", False, True)[2]
+    assert (np.abs(got - want) <= tol * (1 + 1e-6)).all()
+    _, g, _, _ = ops.xent(fx, fw, labels, fd)
+    known = np.flatnonzero((labels >= 0) & (labels < vocab))
+    own = np.zeros_like(g)
+    own[known, labels[known]] = np.abs(g[known, labels[known]])
+    # of the label's entries 2^-8 becomes 2^-16 (the rest, rounded from fp32), everything else as it was
+    lesser = tol - (own.T @ np.abs(fx)) * (2.0 ** -8 - 2.0 ** -16)
+    assert (np.abs(got - want) <= lesser * (1 + 1e-6)).all()
+
+
 @pytest.mark.parametrize("rows,vocab", [(6, 1000), (300, 1300)])
 def test_logits_of_minus_infinity(rows, vocab):
     """They have probability 0; a row with such a label has an infinite loss."""
