@@ -228,7 +228,9 @@ struct XentArgs {
 // (74 on 128 x 128, 82 on 256 x 256, 103 on 64 x 128), 1024 x 32000 x 4096 197 on 256 x
 // 256 (230 on 256 x 128).  Loss with dX: 200 x 32000 x 4096 172 on 64 x 256 shared by
 // four workgroups (176 on 128 x 256, 216 on 256 x 256, 383 unshared), 512 x 32003 x 4096
-// 249 on 256 x 256 shared by eight (262 on 128 x 256 by four, 311 on 64 x 256).
+// 249 on 256 x 256 shared by eight (262 on 128 x 256 by four, 311 on 64 x 256).  dW of a
+// piece: with its gradient of 8192 x 32000 x 1024, whose pieces are 64 tiles of 256 x 256,
+// the two-call backward takes 1670 us on 64 x 256 and 2270 on 256 x 256.
 enum XentTileKind { XENT_64x128, XENT_128x128, XENT_256x128, XENT_256x256 };
 enum XentGradKind { XENT_GRAD_64x256, XENT_GRAD_128x256, XENT_GRAD_256x256 };
 constexpr TileCost kXentTiles[4] = {{XENT_64x128, 64, 128, 256, 3.0, 0.45, 0.62},
@@ -252,6 +254,7 @@ struct XentPlan {
   int vtiles, piece_tiles, pieces;   // tiles of the vocabulary, of a piece
   int64_t rows_pad, piece;     // padded rows, columns of a piece (its row pitch)
   int tiles_k, splits;         // column tiles of dX, parts of a piece that workgroups share
+  int dw_kind, dw_m;           // a piece's dW: XentGradKind, its rows
   int64_t stages;              // 64-column stages of a piece
   bool local;                  // the one-pass call takes a tile's powers against the tile's own largest
 };
@@ -308,6 +311,15 @@ inline XentPlan plan_xent(int64_t rows, int64_t vocab, int64_t k) {
         p.grad_tiles_m = (int)tm;
         p.splits = (int)splits;
       }
+    }
+  }
+  least = 1e30;
+  for (const TileCost& t : kXentGradTiles) {
+    const double time = tile_time(t, cdiv(std::min(p.piece, vocab), t.bm) * p.tiles_k, (double)cdiv(rows, 64));
+    if (time < least) {
+      least = time;
+      p.dw_kind = t.kind;
+      p.dw_m = t.bm;
     }
   }
   p.local = p.pieces == 1 && p.grad_kind != XENT_GRAD_256x256 &&

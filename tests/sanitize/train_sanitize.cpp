@@ -139,7 +139,7 @@ int main(int argc, char** argv) {
       const int64_t m = atoll(argv[i]), n = atoll(argv[i + 1]), k = atoll(argv[i + 2]);
       if (strcmp(argv[1], "xent") == 0) {   // rows, vocab, k: its kernels, and whether there are parts to join and pieces
         const lora::XentPlan p = lora::plan_xent(m, n, k);
-        printf("logits%d grad%d join%d pieces%d local%d\n", p.kind, p.grad_kind, p.splits > 1 ? p.grad_kind : -1, p.pieces > 1, p.local ? p.grad_kind : -1);
+        printf("logits%d grad%d join%d pieces%d local%d dw%d\n", p.kind, p.grad_kind, p.splits > 1 ? p.grad_kind : -1, p.pieces > 1, p.local ? p.grad_kind : -1, p.dw_kind);
         continue;
       }
       const lora::Fp8Plan p = strcmp(argv[1], "fwd") == 0 ? lora::plan_fp8_fwd(m, n, k) : lora::plan_fp8_bwd(m, n, k);

@@ -57,5 +57,5 @@ def test_gpu_sizes_reach_every_kernel_of_the_loss(driver):
     sizes = [str(x) for shape in gpu.SIZES + [(4100, 20011, 72)] for x in shape]
     text = _run([driver, "xent"] + sizes, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
     want = {f"logits{i}" for i in range(4)} | {f"grad{i}" for i in range(3)} | {f"join{i}" for i in range(3)} | \
-        {"join-1", "pieces0", "pieces1", "local-1", "local0", "local1"}
+        {"join-1", "pieces0", "pieces1", "local-1", "local0", "local1", "dw0", "dw1", "dw2"}
     assert set(text.split()) == want
