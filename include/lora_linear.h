@@ -571,7 +571,7 @@ lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtyp
  *             (0 on invalid arguments; dx, dw: whether the call writes dX, dW; both 0
  *             for the forward; a call with fewer outputs needs no more), 16-byte
  *             aligned, not used concurrently
- * Logits, their exponentials and all sums are fp32; G enters its products as bf16, the
+ * Logits, their exponentials and all sums are fp32, the label's logit in the loss fp64; G enters its products as bf16, the
  * label's entry with what that loses added apart.
  * A row with a label and a NaN or plus infinity among its logits has loss and dX NaN,
  * and so has dW; minus infinity is a logit of probability 0 (of the label: an infinite

@@ -330,7 +330,6 @@ inline XentPlan plan_xent(int64_t rows, int64_t vocab, int64_t k) {
 }
 // Regions of the workspace.
 struct XentLayout {
-  size_t zy;       // [rows_pad] the labels' logits
   size_t coef;     // [rows_pad][2] dX = c1 sum_v e_v W_v + c2 W_label
   size_t ref;      // [2][rows_pad] references of the exponentials, of a piece and the next
   size_t best;     // [2][rows_pad] a piece's largest logits
@@ -345,8 +344,7 @@ struct XentLayout {
 inline XentLayout xent_layout(int64_t rows, int64_t vocab, int64_t k, bool dx, bool dw) {
   const XentPlan p = plan_xent(rows, vocab, k);
   XentLayout L;
-  L.zy = 0;
-  L.coef = L.zy + region((size_t)p.rows_pad * 4);
+  L.coef = 0;
   L.ref = L.coef + region((size_t)p.rows_pad * 8);
   L.best = L.ref + region((size_t)p.rows_pad * 8);
   L.parts = L.best + region((size_t)p.rows_pad * 8);

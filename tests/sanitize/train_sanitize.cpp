@@ -120,7 +120,7 @@ static int plans() {
         size_t last = 0;
         for (int d = 0; d < 4; ++d) {
           const XentLayout L = xent_layout(rows, vocab, k, d & 1, d >> 1);
-          HOLDS(L.coef - L.zy >= (size_t)p.rows_pad * 4 && L.ref - L.coef >= (size_t)p.rows_pad * 8 && L.best - L.ref >= (size_t)p.rows_pad * 8 && L.parts - L.best >= (size_t)p.rows_pad * 8 && L.parts <= L.piece && L.piece <= L.turned && L.turned <= L.known && L.known <= L.sums && L.sums <= L.saved && L.saved <= L.total, rows, vocab, k);
+          HOLDS(L.ref - L.coef >= (size_t)p.rows_pad * 8 && L.best - L.ref >= (size_t)p.rows_pad * 8 && L.parts - L.best >= (size_t)p.rows_pad * 8 && L.parts <= L.piece && L.piece <= L.turned && L.turned <= L.known && L.known <= L.sums && L.sums <= L.saved && L.saved <= L.total, rows, vocab, k);
           HOLDS(L.piece - L.parts >= (size_t)(p.vtiles * p.rows_pad * 8), rows, vocab, k);
           if (d) HOLDS(L.turned - L.piece >= (size_t)(p.rows_pad * p.piece * 2), rows, vocab, k);
           if (d & 2) HOLDS(L.known - L.turned >= (size_t)(p.rows_pad * p.piece * 2) && L.sums - L.known >= (size_t)(rows * k * 2) && L.total - L.saved >= (size_t)(rows * 8), rows, vocab, k);

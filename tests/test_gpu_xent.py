@@ -195,6 +195,28 @@ def test_labels_rows_of_dW(rows, vocab, k, spread):
     assert (np.abs(got - want) <= lesser * (1 + 1e-6)).all()
 
 
+@pytest.mark.parametrize("rows,vocab,k", [(5, 1000, 4096), (300, 3001, 5000), (70, 2, 1032)])
+def test_labels_logit_is_exact(rows, vocab, k):
+    """All other logits 0, the label's a sum of k terms that cancel: the loss is off by its
+    own rounding and that of the sum of powers alone, not by an fp32 sum over k."""
+    x, w, labels, d = case(rows, vocab, k, k, spread=1.0, sure=0.0)
+    w = f64(w) * 16
+    y = vocab // 2
+    w[:y], w[y + 1:] = 0, 0
+    w, labels = to_bits(w), np.full(rows, y, np.int32)
+    z = f64(x) @ f64(w)[y]
+    want = np.where(z > 0, np.log1p((vocab - 1) * np.exp(-z)), np.log(vocab - 1 + np.exp(np.minimum(z, 0))) - z)   # (no cancellation)
+    assert want.max() > 16
+    # the sum of powers, its rounding and the label's power: 2^-24 of it each (vocab - 1 is exact), a
+    # power whose exponent was rounded to 2^-24 of at most 128, and a small loss's quotient
+    # and logarithm: 2^-22 of it; the result's rounding
+    unlikely = z < 0
+    tol = np.where(unlikely, 4 * 2.0 ** -24 + 2.0 ** -24 * want, 2.0 ** -17 * want)
+    for how in ("step", "two"):
+        loss = run(x, w, labels, d, how)[0]
+        assert (np.abs(loss - want) <= tol * (1 + 1e-6)).all(), how
+
+
 @pytest.mark.parametrize("rows,vocab", [(6, 1000), (300, 1300)])
 def test_logits_of_minus_infinity(rows, vocab):
     """They have probability 0; a row with such a label has an infinite loss."""
