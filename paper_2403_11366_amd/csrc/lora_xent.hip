@@ -14,7 +14,8 @@
 // and divided at the end.  r is 0 until a piece's largest logit is more than 64
 // above it or, in the first piece, more than 40 below it (in powers of two; bf16 and
 // fp32 hold 2^126): then the tiles of those rows are formed again against the
-// maximum, and what is carried is scaled.  So any logits come out right, and
+// maximum, and what is carried is scaled.  (A piece whose logits all have probability 0 in
+// a row leaves the next one that row's first.)  So any logits come out right, and
 // ordinary ones at the price of two products and, for each piece, of a launch that
 // finds nothing to do (4 us).  For few rows, whose piece is the whole vocabulary, that
 // launch and the references' are saved: a tile's powers are taken against its own
@@ -80,10 +81,14 @@ __device__ __forceinline__ uint32_t ordered(float f) {
 __device__ __forceinline__ float from_ordered(uint32_t u) {
   return __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
 }
-// The reference that serves a row whose largest logit in a piece is `best`.
-__device__ __forceinline__ float served_by(float ref, float best, bool first) {
-  const bool high = best > ref + 64.0f && best < INFINITY, low = first && best < ref - 40.0f && best > kLowest;
-  return high || low ? ceilf(best) : ref;
+// The reference that serves a row whose largest logit in a piece is `best`.  A row that
+// has met no logit above kLowest has the reference kNoLogit, a 0 apart by its sign: its
+// sums are 0, so that it may still move down.
+constexpr float kNoLogit = -0.0f;
+__device__ __forceinline__ float served_by(float ref, float best) {
+  const bool none = __builtin_bit_cast(uint32_t, ref) == 0x80000000u, some = best > kLowest;
+  const bool high = best > ref + 64.0f && best < INFINITY, low = none && some && best < ref - 40.0f;
+  return high || low ? ceilf(best) : (none && some ? 0.0f : ref);
 }
 
 // One tile of logits: the product's sums are what the epilogue works on, in registers;
@@ -260,7 +265,7 @@ __global__ __launch_bounds__(NT) void lora_xent_logits_kernel(XentLogits p) {
       lds.label[i] = known ? y : -1;
       if (MODE == XENT_PIECE) lds.ref[i] = p.ref[row];
       if (MODE == XENT_AGAIN) {
-        const float old = p.ref[row], ref = row < p.rows ? served_by(old, from_ordered(p.best[row]), p.tile0 == 0) : old;
+        const float old = p.ref[row], ref = row < p.rows ? served_by(old, from_ordered(p.best[row])) : old;
         again = again || ref != old;
         lds.ref[i] = ref;
         if (tn == 0) {
@@ -349,8 +354,8 @@ __global__ __launch_bounds__(256) void lora_xent_rows_kernel(const Part* __restr
   }
   Part v{kLowest, 0.0f};
   auto add = [&](Part u) LORA_INLINE {
-    const float m = fmaxf(v.m, u.m);
-    v.s = v.s * __builtin_amdgcn_exp2f(v.m - m) + u.s * __builtin_amdgcn_exp2f(u.m - m);
+    const float m = fmaxf(v.m, u.s == 0.0f ? kLowest : u.m);   // (a tile without a power may stand against any reference)
+    v.s = v.s * __builtin_amdgcn_exp2f(v.m - m) + (u.s == 0.0f ? 0.0f : u.s * __builtin_amdgcn_exp2f(u.m - m));
     v.m = m;
   };
   for (int t = tid / RB; t < tiles; t += 4 * PER) {
@@ -388,7 +393,7 @@ __global__ __launch_bounds__(256) void lora_xent_rows_kernel(const Part* __restr
 __global__ __launch_bounds__(256) void lora_xent_begin_kernel(float* ref, uint32_t* best, int64_t rows_pad) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= rows_pad) return;
-  ref[i] = 0.0f;
+  ref[i] = kNoLogit;
   best[i] = ordered(kLowest);
 }
 
@@ -548,7 +553,8 @@ __global__ __launch_bounds__(NT) void lora_xent_grad_kernel(XentGrad p) {
 #pragma unroll
   for (int b = 0; b < FB; ++b) {
     const int row = m0 + Core::row0(wave) + 16 * b + c16;
-    const float alpha = !LOCAL && !p.first && p.ref ? __builtin_amdgcn_exp2f(p.ref_old[row] - p.ref[row]) : 1.0f;
+    // (a reference moves down where nothing is carried: 1)
+    const float alpha = !LOCAL && !p.first && p.ref ? __builtin_amdgcn_exp2f(fminf(p.ref_old[row] - p.ref[row], 0.0f)) : 1.0f;
 #pragma unroll
     for (int a = 0; a < FA; ++a) {
       floatx4 v = acc[a][b];
