@@ -572,7 +572,9 @@ lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtyp
  *             for the forward; a call with fewer outputs needs no more), 16-byte
  *             aligned, not used concurrently
  * Logits, their exponentials and all sums are fp32, the label's logit in the loss fp64; G enters its products as bf16, the
- * label's entry with what that loses added apart.
+ * label's entry with what that loses added apart.  A finite logit of any size counts (a mask of -1e10 as of the lowest
+ * value); where the logarithm of a row's sum passes 2^16 in size, `saved` holds the row's normaliser and label's entry to
+ * bf16.
  * A row with a label and a NaN or plus infinity among its logits has loss and dX NaN,
  * and so has dW; minus infinity is a logit of probability 0 (of the label: an infinite
  * loss), whose entry of dX is 0 times a W that is not finite.  rows >= 1, vocab >= 1, k >= 8 and a multiple of 8 (LORA_ERR_SHAPE), rows and

@@ -10,10 +10,10 @@
 //
 // One call for loss and dX (lora_xent_step without dW) forms the logits once: a
 // piece's exponentials are taken against a reference r of each row instead of its
-// normaliser, sum_v 2^(z_v log2 e - r) W_v is carried from piece to piece in fp32,
-// and divided at the end.  r is 0 until a piece's largest logit is more than 64
-// above it or, in the first piece, more than 40 below it (in powers of two; bf16 and
-// fp32 hold 2^126): then the tiles of those rows are formed again against the
+// normaliser, sum_v e^(z_v - r) W_v is carried from piece to piece in fp32,
+// and divided at the end.  r is 0 until a piece's largest logit is more than 44
+// above it or, in the first piece, more than 28 below it (e^44 is 2^63, e^-28 2^-40;
+// bf16 and fp32 hold 2^126): then the tiles of those rows are formed again against the
 // maximum, and what is carried is scaled.  (A piece whose logits all have probability 0 in
 // a row leaves the next one that row's first.)  So any logits come out right, and
 // ordinary ones at the price of two products and, for each piece, of a launch that
@@ -31,7 +31,10 @@
 // largest error of dW by far (1500 x 50021: error against 64 bits 0.0022 -> 0.0017 of the
 // result, the plain form's).
 //
-// Exponents are in powers of two: v_exp_f32 of fma(z, log2 e, -r).
+// References are logits, and a power is v_exp_f32 of (z - r) log2 e: the difference first,
+// so that a logit that is its own reference has the power 1 however large it is.  (A
+// reference in rounded powers of two is off by 2^-24 of itself, and from 1e9 on that is
+// more than fp32's exponents: a masked tile at -1e10 made its row's sum infinite.)
 //
 // What bounds it: with many rows the two (with dW four) products, on the matrix cores --
 // loss and dX of 4096 rows, vocabulary 32000, k 4096 in 1.56 ms, the two products alone
@@ -47,12 +50,53 @@
 
 namespace lora {
 
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLowest = -1e30f;   // below any logit that counts
+constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.925963033500e-8f;   // log2 e = their sum
+constexpr float kLowest = -3.4028234663852886e38f;   // the lowest finite logit
+constexpr float kNone = -INFINITY;                   // the largest of no logits
 
 struct Part {   // of a row's logits in a tile: reference, sum of powers against it
   float m, s;
 };
+__device__ __forceinline__ float power(float z, float ref) { return __builtin_amdgcn_exp2f((z - ref) * kLog2e); }
+
+// References of a tile's own (XENT_LOCAL): the power of two next to e^top, so that a tile's
+// powers differ from another's by a whole exponent.  2^(t log2 e + c): from 2^28 on, where
+// different logits lie 46 powers and more apart, e^top itself.
+struct Whole {
+  float t, c;
+};
+__device__ __forceinline__ Whole whole_power(float top) {
+  return fabsf(top) < 268435456.0f ? Whole{0.0f, ceilf(top * kLog2e)} : Whole{top, 0.0f};
+}
+// log2 of e^top over that reference: about -1 .. 0.
+__device__ __forceinline__ float past_whole(float top) {
+  const Whole w = whole_power(top);
+  return fmaf(top - w.t, kLog2e, -w.c) + (top - w.t) * kLog2eLow;
+}
+// By how many powers of two the reference of m is above that of top, m >= top.
+__device__ __forceinline__ float powers_above(float m, float top) {
+  const Whole a = whole_power(m), b = whole_power(top);
+  return ceilf(fmaf(a.t - b.t, kLog2e, a.c - b.c));
+}
+
+// What a row's backward reads: log sum e^z and 1 - p of its label.  From 2^16 on, where the
+// logarithm's spacing shows in e^(z - it), instead the largest logit but the label's, and
+// 1 - p and what powers against that logit are multiplied by, each as bf16 and apart by
+// the sign (1 - p has none).
+struct Saved {
+  float ref, scale, rest;
+};
+__device__ __forceinline__ void save_row(float* to, float lse, const Saved& wide) {
+  const bool far = fabsf(lse) >= 65536.0f;
+  const uint32_t both = 0x80000000u | (uint32_t)f32_to_bf16(wide.rest) << 16 | f32_to_bf16(wide.scale);
+  to[0] = far ? wide.ref : lse;
+  to[1] = far ? __builtin_bit_cast(float, both) : wide.rest;
+}
+__device__ __forceinline__ Saved saved_row(const float* at) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, at[1]);
+  if (!(b >> 31)) return Saved{at[0], 1.0f, at[1]};
+  return Saved{at[0], bf16_to_f32((u16)b), bf16_to_f32((u16)(b >> 16 & 0x7FFFu))};
+}
 
 enum XentMode { XENT_STATS, XENT_PIECE, XENT_AGAIN, XENT_LOCAL, XENT_GRAD };
 
@@ -82,13 +126,13 @@ __device__ __forceinline__ float from_ordered(uint32_t u) {
   return __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
 }
 // The reference that serves a row whose largest logit in a piece is `best`.  A row that
-// has met no logit above kLowest has the reference kNoLogit, a 0 apart by its sign: its
+// has met no finite logit has the reference kNoLogit, a 0 apart by its sign: its
 // sums are 0, so that it may still move down.
 constexpr float kNoLogit = -0.0f;
 __device__ __forceinline__ float served_by(float ref, float best) {
-  const bool none = __builtin_bit_cast(uint32_t, ref) == 0x80000000u, some = best > kLowest;
-  const bool high = best > ref + 64.0f && best < INFINITY, low = none && some && best < ref - 40.0f;
-  return high || low ? ceilf(best) : (none && some ? 0.0f : ref);
+  const bool none = __builtin_bit_cast(uint32_t, ref) == 0x80000000u, some = best > kNone;
+  const bool high = best > ref + 44.0f && best < INFINITY, low = none && some && best < -28.0f;
+  return high || low ? best : (none && some ? 0.0f : ref);
 }
 
 // One tile of logits: the product's sums are what the epilogue works on, in registers;
@@ -140,21 +184,22 @@ struct XentTile {
       constexpr int b = decltype(bc)::value;
       constexpr bool PLAIN = decltype(plain)::value;
       const int i = r0 + 16 * b + c16, y = lds.label[i];
-      const float r = MODE == XENT_STATS ? 0.0f : lds.ref[i];
+      float r = MODE == XENT_STATS ? 0.0f : lds.ref[i];
       if constexpr (MODE != XENT_GRAD) {
-        float top = MODE == XENT_LOCAL ? -INFINITY : largest(bc, plain), base = r;
+        float top = kNone;
         if constexpr (MODE == XENT_STATS || MODE == XENT_PIECE) {
+          top = largest(bc, plain);
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          top = fmaxf(top * kLog2e, kLowest);
-          if (MODE == XENT_STATS) base = top;
+          if (MODE == XENT_STATS) r = top = fmaxf(top, kLowest);
         }
+        const float past = MODE == XENT_LOCAL ? past_whole(r) : 0.0f;
         float sum = 0.0f;
 #pragma unroll
         for (int a = 0; a < FA; ++a)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            float v = __builtin_amdgcn_exp2f(fmaf(acc[a][b][q], kLog2e, -base));
+            float v = MODE == XENT_LOCAL ? __builtin_amdgcn_exp2f(fmaf(acc[a][b][q] - r, kLog2e, past)) : power(acc[a][b][q], r);
             if constexpr (!PLAIN) {
               const int col = n0 + Core::col(wave, a) + 4 * g + q;
               v = col < p.vocab && col != y ? v : 0.0f;
@@ -171,7 +216,7 @@ struct XentTile {
         for (int a = 0; a < FA; ++a)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            float v = d * __builtin_amdgcn_exp2f(fmaf(acc[a][b][q], kLog2e, -r));
+            float v = d * power(acc[a][b][q], r);
             v = y < 0 ? 0.0f : v;
             if constexpr (!PLAIN) {
               const int col = n0 + Core::col(wave, a) + 4 * g + q;
@@ -199,7 +244,7 @@ struct XentTile {
         float top = lds.joined[0][i].m;
 #pragma unroll
         for (int w = 1; w < WN; ++w) top = fmaxf(top, lds.joined[w][i].m);
-        lds.ref[i] = ceilf(fmaxf(top * kLog2e, kLowest));
+        lds.ref[i] = fmaxf(top, kLowest);
       }
       __syncthreads();
     }
@@ -216,11 +261,14 @@ struct XentTile {
         for (int w = 1; w < WN; ++w) {
           const Part u = lds.joined[w][i];
           const float m = fmaxf(v.m, u.m);
-          v.s = MODE == XENT_STATS ? v.s * __builtin_amdgcn_exp2f(v.m - m) + u.s * __builtin_amdgcn_exp2f(u.m - m) : v.s + u.s;
+          v.s = MODE == XENT_STATS ? v.s * power(v.m, m) + u.s * power(u.m, m) : v.s + u.s;
           v.m = m;
         }
-        if (MODE == XENT_PIECE && v.m > kLowest) atomicMax(p.best + m0 + i, ordered(v.m));
-        p.parts[(size_t)(p.tile0 + tn) * p.rows_pad + m0 + i] = Part{EXPS ? lds.ref[i] : v.m, v.s};
+        if (MODE == XENT_PIECE && v.m > kNone) atomicMax(p.best + m0 + i, ordered(v.m));
+        if (EXPS) v.m = lds.ref[i];
+        if (MODE == XENT_LOCAL) v.s *= __builtin_amdgcn_exp2f(-past_whole(v.m));
+        if (v.s == 0.0f) v.m = kLowest;   // no power: its reference does not count
+        p.parts[(size_t)(p.tile0 + tn) * p.rows_pad + m0 + i] = v;
       }
     }
     if constexpr (MODE != XENT_STATS) {
@@ -270,14 +318,15 @@ __global__ __launch_bounds__(NT) void lora_xent_logits_kernel(XentLogits p) {
         lds.ref[i] = ref;
         if (tn == 0) {
           p.ref_next[row] = ref;
-          p.best_next[row] = ordered(kLowest);
+          p.best_next[row] = ordered(kNone);
         }
       }
       if (MODE == XENT_GRAD) {
+        const Saved row_of = known ? saved_row(p.saved + 2 * row) : Saved{0.0f, 0.0f, 0.0f};
         const float d = known ? p.dloss[row] : 0.0f;
-        lds.ref[i] = known ? p.saved[2 * row] : 0.0f;
-        lds.scale[i] = d;
-        const float o = known ? -d * p.saved[2 * row + 1] : 0.0f;
+        lds.ref[i] = row_of.ref;
+        lds.scale[i] = d * row_of.scale;
+        const float o = known ? -d * row_of.rest : 0.0f;
         lds.own[i] = o;
         if (p.coef && tn == 0) {   // for dX and dW: what the label's entry of G loses as bf16
           p.coef[2 * row] = 1.0f;
@@ -297,20 +346,20 @@ __global__ __launch_bounds__(NT) void lora_xent_logits_kernel(XentLogits p) {
 // the tile's fp32 sum the loss of 7 x 2000 x 5120 was off by 1.9e-6 (rms), now by 5e-7,
 // at 0.3% (4096 x 32000 x 4096) to 4% (37 rows) of the call's time.
 struct RowEnd {
-  float loss, lse, rest;   // lse in powers of two; rest = 1 - p_label
+  float loss, lse, rest;   // rest = 1 - p_label
   float c1;                // 1 / sum, against ref
 };
 __device__ __forceinline__ RowEnd row_end(float ref, float others, double zy, bool known) {
   RowEnd e;
   if (!(fabs(zy) <= 3.4028234663852886e38)) zy = (double)(float)zy;   // infinite as a logit is
-  const double dy = known ? zy * 1.4426950408889634074 - (double)ref : -(double)INFINITY, up = fmax(dy, 0.0);   // (NaN: 0, and dy below)
+  const double dy = known ? (zy - (double)ref) * 1.4426950408889634074 : -(double)INFINITY, up = fmax(dy, 0.0);   // (NaN: 0, and dy below)
   const double whole = floor(up);
   const float down = up < 1000.0 ? ldexpf(__builtin_amdgcn_exp2f((float)(whole - up)), -(int)whole) : 0.0f, rest = others * down;
   const float ey = known ? __builtin_amdgcn_exp2f((float)(dy - up)) : 0.0f, sum = rest + ey;
   const float bad = sum < INFINITY ? 0.0f : NAN;   // a NaN or an infinity among the logits
   const double log = log2((double)sum);
   e.loss = known ? (ey > rest ? log1pf(rest / ey) : (float)(0.69314718055994530942 * (log - (dy - up)))) + bad : 0.0f;
-  e.lse = (float)((double)ref + up + log) + bad;
+  e.lse = (float)((double)ref + 0.69314718055994530942 * (up + log)) + bad;
   e.rest = known ? rest / sum + bad : 0.0f;
   e.c1 = known ? down / sum + bad : 0.0f;
   return e;
@@ -318,8 +367,8 @@ __device__ __forceinline__ RowEnd row_end(float ref, float others, double zy, bo
 
 // Joins the tiles' parts of 4 rows, 64 threads a row, in a fixed order, and forms the
 // label's logit in fp64 (a row of X, a row of W).  The
-// forward keeps lse and rest in `saved` (or nowhere), the one-pass call c1 and c2 in
-// `coef` and, with local references, the largest of them in `ref`.
+// forward keeps what Saved says in `saved` (or nowhere), the one-pass call c1 and c2 in
+// `coef` and, with tiles' own references, the largest tile's logit in `ref` (else none).
 constexpr int kRowsPer = 4;
 __global__ __launch_bounds__(256) void lora_xent_rows_kernel(const Part* __restrict__ parts, const u16* __restrict__ X,
                                                              const u16* __restrict__ W, const int32_t* __restrict__ labels,
@@ -354,8 +403,8 @@ __global__ __launch_bounds__(256) void lora_xent_rows_kernel(const Part* __restr
   }
   Part v{kLowest, 0.0f};
   auto add = [&](Part u) LORA_INLINE {
-    const float m = fmaxf(v.m, u.s == 0.0f ? kLowest : u.m);   // (a tile without a power may stand against any reference)
-    v.s = v.s * __builtin_amdgcn_exp2f(v.m - m) + (u.s == 0.0f ? 0.0f : u.s * __builtin_amdgcn_exp2f(u.m - m));
+    const float m = fmaxf(v.m, u.m);
+    v.s = v.s * power(v.m, m) + u.s * power(u.m, m);
     v.m = m;
   };
   for (int t = tid / RB; t < tiles; t += 4 * PER) {
@@ -379,13 +428,10 @@ __global__ __launch_bounds__(256) void lora_xent_rows_kernel(const Part* __restr
   if (row >= rows) return;
   const RowEnd e = row_end(v.m, v.s, dot, known);
   loss[row] = e.loss;
-  if (saved) {
-    saved[2 * row] = e.lse;
-    saved[2 * row + 1] = e.rest;
-  }
+  if (saved) save_row(saved + 2 * row, e.lse, Saved{v.m, e.c1, e.rest});
   if (coef) {
-    const float d = known ? dloss[row] : 0.0f;
-    coef[2 * row] = known ? d * e.c1 : 0.0f;
+    const float d = known ? dloss[row] : 0.0f, c1 = ref ? e.c1 * __builtin_amdgcn_exp2f(-past_whole(v.m)) : e.c1;
+    coef[2 * row] = known ? d * c1 : 0.0f;
     coef[2 * row + 1] = known ? -d * e.rest : 0.0f;
   }
 }
@@ -394,7 +440,7 @@ __global__ __launch_bounds__(256) void lora_xent_begin_kernel(float* ref, uint32
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= rows_pad) return;
   ref[i] = kNoLogit;
-  best[i] = ordered(kLowest);
+  best[i] = ordered(kNone);
 }
 
 // X for dW: rows without a label are 0 there, whatever they hold (G is, and its product
@@ -541,7 +587,7 @@ __global__ __launch_bounds__(NT) void lora_xent_grad_kernel(XentGrad p) {
     const int first = s0 >> p.tile_log, count = s1 > s0 ? ((s1 - 1) >> p.tile_log) - first + 1 : 0;
     for (int i = threadIdx.x; i < min(count, LT) * BM; i += NT) {
       const int row = m0 + i % BM;
-      const float d = p.ref[row] - p.parts[(size_t)(first + i / BM) * p.rows_pad + row].m;
+      const float d = powers_above(p.ref[row], p.parts[(size_t)(first + i / BM) * p.rows_pad + row].m);
       table[i] = d < 255.0f ? (u16)((int)d << 7) : (u16)(255 << 7);   // (a NaN: 255, and the row's result is one)
     }
     Core::template run<true>(t, Scales{}, m0, s0, s1, smem, acc, Shifts<BM>{table, first, p.tile_log});
@@ -553,12 +599,16 @@ __global__ __launch_bounds__(NT) void lora_xent_grad_kernel(XentGrad p) {
 #pragma unroll
   for (int b = 0; b < FB; ++b) {
     const int row = m0 + Core::row0(wave) + 16 * b + c16;
-    // (a reference moves down where nothing is carried: 1)
-    const float alpha = !LOCAL && !p.first && p.ref ? __builtin_amdgcn_exp2f(fminf(p.ref_old[row] - p.ref[row], 0.0f)) : 1.0f;
+    // (a reference moves down where nothing is carried: 1; and 0 times a masked part's sum, which may be infinite, is 0)
+    const float alpha = !LOCAL && !p.first && p.ref ? power(fminf(p.ref_old[row], p.ref[row]), p.ref[row]) : 1.0f;
 #pragma unroll
     for (int a = 0; a < FA; ++a) {
       floatx4 v = acc[a][b];
-      if (!p.first) v += to[(a * FB + b) * NT] * alpha;
+      if (!p.first) {
+        const floatx4 carried = to[(a * FB + b) * NT];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += alpha == 0.0f ? 0.0f : carried[q] * alpha;
+      }
       if (END == XENT_CARRY) to[(a * FB + b) * NT] = v;
       if (END == XENT_LABEL) v = with_label(v, p.coef, p.labels, p.W, row, p.rows, p.vocab, p.k, l0 + Core::col(wave, a) + 4 * g);
       acc[a][b] = v;
