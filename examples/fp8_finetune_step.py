@@ -24,7 +24,8 @@ BF16 = dict(dtype=torch.bfloat16, device="cuda")
 
 
 class EightBitLayer:
-    """A frozen weight [n, k] held in 8 bits, and what a step's calls on it need."""
+    """A frozen weight [n, k] held in 8 bits, and what a step's calls on it need for up to
+    `tokens` tokens."""
 
     def __init__(self, W: torch.Tensor, tokens: int):
         n, k = W.shape
@@ -54,7 +55,8 @@ class EightBitLayer:
 
 
 class Model:
-    """hidden = X + dropout(W1 X + s B A X);  logits = W3 (W2 hidden)."""
+    """hidden = X + dropout(W1 X + s B A X);  logits = W3 (W2 hidden).  Steps of up to
+    `tokens` tokens."""
 
     def __init__(self, tokens: int, features: int, vocab: int, rank: int, p: float, seed: int):
         gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -78,20 +80,21 @@ class Model:
     def step(self, X: torch.Tensor, labels: torch.Tensor, seed: int):
         """Losses of the tokens, and the adapter's gradients of their mean over labelled tokens."""
         m, k = X.shape
+        U, loss = self.U[:m], self.loss[:m]
         Y, hidden = torch.empty((m, k), **BF16), torch.empty((m, k), **BF16)
-        lora.lora_linear_fwd(X, self.up_bf16, self.A, self.B, Y, self.U, self.alpha)
+        lora.lora_linear_fwd(X, self.up_bf16, self.A, self.B, Y, U, self.alpha)
         lora.lora_dropout(Y, hidden, seed, self.counter, self.p, residual=X)
         out = self.down.forward(hidden)
         labelled = (labels >= 0) & (labels < self.head.shape[0])
         dloss = labelled.float() / labelled.sum()
         dout = torch.empty((m, k), **BF16)
-        lora.lora_linear_xent_step(out, self.head, labels, dloss, self.loss, dout, None, self.ws_loss)
+        lora.lora_linear_xent_step(out, self.head, labels, dloss, loss, dout, None, self.ws_loss)
         dhidden = self.down.backward(dout)
         dY, dX = torch.empty((m, k), **BF16), torch.empty((m, k), **BF16)
         lora.lora_dropout(dhidden, dY, seed, self.counter, self.p)     # the same elements as the forward's
-        lora.lora_linear_bwd(dY, X, self.up_bf16, self.A, self.B, self.U, dX, self.dA, self.dB, self.ws_lora, self.alpha)
+        lora.lora_linear_bwd(dY, X, self.up_bf16, self.A, self.B, U, dX, self.dA, self.dB, self.ws_lora, self.alpha)
         self.counter += (m * k + 15) // 16
-        return self.loss, self.dA, self.dB
+        return loss, self.dA, self.dB
 
 
 def train(tokens: int = 512, features: int = 512, vocab: int = 8000, rank: int = 8, steps: int = 20, p: float = 0.05,

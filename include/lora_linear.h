@@ -517,7 +517,8 @@ lora_status lora_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, lor
  *   W_codes, W_scales   of W [n, k], read only
  *   Y, dY     [m, n] bf16
  *   workspace at least lora_linear_fp8_fwd_workspace_size(m, n, k), or ..._bwd_...,
- *             bytes (0 on an invalid shape), 16-byte aligned, not used concurrently
+ *             bytes (0 on an invalid shape), which serve every smaller m too; 16-byte
+ *             aligned, not used concurrently
  * The rules above apply to X, W and Y.  A block of an operand with a NaN or an
  * infinity makes every output that it enters NaN.
  */
@@ -569,8 +570,8 @@ lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtyp
  *   dX, dW    [rows, k], [vocab, k] bf16, written; one of them may be NULL
  *   workspace at least lora_linear_xent_workspace_size(rows, vocab, k, dx, dw) bytes
  *             (0 on invalid arguments; dx, dw: whether the call writes dX, dW; both 0
- *             for the forward; a call with fewer outputs needs no more), 16-byte
- *             aligned, not used concurrently
+ *             for the forward; a call with fewer outputs or fewer rows needs no
+ *             more), 16-byte aligned, not used concurrently
  * Logits, their exponentials and all sums are fp32, the label's logit in the loss fp64; G enters its products as bf16, the
  * label's entry with what that loses added apart.  A finite logit of any size counts (a mask of -1e10 as of the lowest
  * value); where the logarithm of a row's sum passes 2^16 in size, `saved` holds the row's normaliser and label's entry to

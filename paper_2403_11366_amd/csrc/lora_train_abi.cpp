@@ -130,11 +130,13 @@ lora_status lora_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, lor
 }
 
 size_t lora_linear_fp8_fwd_workspace_size(int64_t m, int64_t n, int64_t k) {
-  return check_linear(m, n, k) == LORA_OK ? lora::fp8_fwd_layout(m, n, k).total : 0;
+  if (check_linear(m, n, k) != LORA_OK) return 0;
+  return lora::bytes_up_to(m, [&](int64_t rows) { return lora::fp8_fwd_layout(rows, n, k).total; });
 }
 
 size_t lora_linear_fp8_bwd_workspace_size(int64_t m, int64_t n, int64_t k) {
-  return check_linear(m, n, k) == LORA_OK ? lora::fp8_bwd_layout(m, n, k).total : 0;
+  if (check_linear(m, n, k) != LORA_OK) return 0;
+  return lora::bytes_up_to(m, [&](int64_t rows) { return lora::fp8_bwd_layout(rows, n, k).total; });
 }
 
 lora_status lora_linear_fp8_fwd(const lora_bf16* X, const uint8_t* W_codes, const uint8_t* W_scales, lora_bf16* Y,
@@ -188,7 +190,8 @@ lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtyp
 }
 
 size_t lora_linear_xent_workspace_size(int64_t rows, int64_t vocab, int64_t k, int dx, int dw) {
-  return check_xent(rows, vocab, k) == LORA_OK ? lora::xent_layout(rows, vocab, k, dx != 0, dw != 0).total : 0;
+  if (check_xent(rows, vocab, k) != LORA_OK) return 0;
+  return lora::bytes_up_to(rows, [&](int64_t r) { return lora::xent_layout(r, vocab, k, dx != 0, dw != 0).total; });
 }
 
 }  // extern "C"
