@@ -497,8 +497,9 @@ lora_status lora_fp8_quantize(const lora_bf16* X, uint8_t* codes, uint8_t* scale
                               int block_rows, void* stream);
 
 /* The values that codes and scales stand for, X [rows, k] (bf16: exact from 2^-126 on;
- * scales above 246, which lora_fp8_quantize does not write, may pass its range to
- * infinity; a code of 127 or 255 is a NaN). */
+ * with scales above 246 they may pass its range to infinity: lora_fp8_quantize writes 247
+ * for blocks above 1.75 2^127, whose elements from 1.9375 2^127 on are nearest to 2^128; a
+ * code of 127 or 255 is a NaN). */
 lora_status lora_fp8_dequantize(const uint8_t* codes, const uint8_t* scales, lora_bf16* X, int64_t rows, int64_t k,
                                 int block_rows, void* stream);
 
