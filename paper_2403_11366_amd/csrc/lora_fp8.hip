@@ -150,7 +150,7 @@ struct Fp8Product {
 };
 
 // ---------------------------------------------------------------------------
-// Few tokens: a workgroup forms 16 FG features x 16 TG tokens with its eight waves on
+// Few tokens: a workgroup forms 16 features x 16 TG tokens with its eight waves on
 // different stages, straight from memory without a barrier until the waves' sums are
 // added, in wave order, through LDS.  A lane loads the two 16-byte chunks of codes
 // that it multiplies; each wave has D stages' loads under way.  Bounded by W's bytes:
@@ -158,40 +158,34 @@ struct Fp8Product {
 // rate; two launches alone 5 to 6), 32 x 11008 x 4096 16.2 us (45 MB, 8.9).
 // From about 32 tokens on tiles in LDS, which read a token's codes once and not once per
 // group of features, take less.
-template <int TG, int FG, int D>
+template <int TG, int D>
 __global__ __launch_bounds__(512) void lora_fp8_few_kernel(Fp8Product p) {
-  constexpr int NW = 8, FR = TG * FG;
-  constexpr int RND = FR < 8 ? FR : 8;   // fragments summed per round
-  __shared__ floatx4 part[NW][RND][64];
+  constexpr int NW = 8;
+  static_assert(TG <= NW, "a wave adds a fragment's sums");
+  __shared__ floatx4 part[NW][TG][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int g = lane >> 4, c = lane & 15;
   int tm, tn;
   tile_coords(p.tiles_m, p.tiles_n, 8, (int)blockIdx.x, tm, tn);
-  const int m0 = tm * 16 * TG, n0 = tn * 16 * FG, stages = (p.k + 127) / 128, cells = (p.m + 63) / 64;
-  const uint8_t *wp[FG], *xp[TG], *xsp[TG];   // rows past the matrix: its last one, not stored
-#pragma unroll
-  for (int f = 0; f < FG; ++f) wp[f] = p.Wc + (size_t)min(n0 + 16 * f + c, p.n - 1) * stages * 128 + 16 * g;
+  const int m0 = tm * 16 * TG, n0 = tn * 16, stages = (p.k + 127) / 128, cells = (p.m + 63) / 64;
+  // rows past the matrix: its last one, not stored
+  const uint8_t* wp = p.Wc + (size_t)min(n0 + c, p.n - 1) * stages * 128 + 16 * g;
+  const uint8_t *xp[TG], *xsp[TG];
 #pragma unroll
   for (int t = 0; t < TG; ++t) {
     const int row = min(m0 + 16 * t + c, p.m - 1);
     xp[t] = p.Ac + (size_t)row * stages * 128 + 16 * g;
     xsp[t] = p.As + fp8_row_scale_at(row, 0, cells);
   }
-  const uint8_t* wsp = p.Ws + (size_t)(n0 / 128) * stages;   // (16 FG features share a block)
-  static_assert(128 % (16 * FG) == 0, "a workgroup's features lie in one block of scales");
-  floatx4 acc[FG][TG];
+  const uint8_t* wsp = p.Ws + (size_t)(n0 / 128) * stages;   // (16 features share a block)
+  floatx4 acc[1][TG];
 #pragma unroll
-  for (int f = 0; f < FG; ++f)
-#pragma unroll
-    for (int t = 0; t < TG; ++t) acc[f][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  Frag w[D][FG], x[D][TG];
+  for (int t = 0; t < TG; ++t) acc[0][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  Frag w[D], x[D][TG];
   int ws[D], xs[D][TG];
   auto load = [&](int j, int s) LORA_INLINE {
-#pragma unroll
-    for (int f = 0; f < FG; ++f) {
-      w[j][f].lo = *reinterpret_cast<const int4v*>(wp[f] + (size_t)s * 128);
-      w[j][f].hi = *reinterpret_cast<const int4v*>(wp[f] + (size_t)s * 128 + 64);
-    }
+    w[j].lo = *reinterpret_cast<const int4v*>(wp + (size_t)s * 128);
+    w[j].hi = *reinterpret_cast<const int4v*>(wp + (size_t)s * 128 + 64);
     ws[j] = wsp[s];
 #pragma unroll
     for (int t = 0; t < TG; ++t) {
@@ -209,27 +203,20 @@ __global__ __launch_bounds__(512) void lora_fp8_few_kernel(Fp8Product p) {
       const int s = s0 + NW * j;
       if (s >= stages) break;
 #pragma unroll
-      for (int t = 0; t < TG; ++t)
-#pragma unroll
-        for (int f = 0; f < FG; ++f) acc[f][t] = stage_product<Fp8, 0>(w[j][f], x[j][t], acc[f][t], ws[j], xs[j][t]);
+      for (int t = 0; t < TG; ++t) acc[0][t] = stage_product<Fp8, 0>(w[j], x[j][t], acc[0][t], ws[j], xs[j][t]);
       if (s + NW * D < stages) load(j, s + NW * D);
     }
   }
   formed(acc);
 #pragma unroll
-  for (int e0 = 0; e0 < FR; e0 += RND) {
-    if (e0) __syncthreads();
+  for (int t = 0; t < TG; ++t) part[wave][t][lane] = acc[0][t];
+  __syncthreads();
+  if (wave < TG) {
+    floatx4 v = part[0][wave][lane];
 #pragma unroll
-    for (int e = 0; e < RND; ++e) part[wave][e][lane] = acc[(e0 + e) % FG][(e0 + e) / FG];
-    __syncthreads();
-    if (wave < RND) {
-      floatx4 v = part[0][wave][lane];
-#pragma unroll
-      for (int q = 1; q < NW; ++q) v += part[q][wave][lane];
-      const int e = e0 + wave, f = e % FG, t = e / FG;
-      const int row = m0 + 16 * t + c, col = n0 + 16 * f + 4 * g;
-      if (row < p.m && col < p.n) *reinterpret_cast<uint2*>(p.out + (size_t)row * p.n + col) = bf16x4(v);
-    }
+    for (int q = 1; q < NW; ++q) v += part[q][wave][lane];
+    const int row = m0 + 16 * wave + c, col = n0 + 4 * g;
+    if (row < p.m && col < p.n) *reinterpret_cast<uint2*>(p.out + (size_t)row * p.n + col) = bf16x4(v);
   }
 }
 
@@ -355,7 +342,7 @@ __global__ __launch_bounds__(NT) void lora_fp8_fwd_kernel(Fp8Product p) {
   const NtTile t{make_rsrc(p.Ac + (size_t)m0 * row + skip, (uint64_t)min(BM, p.m - m0) * row - skip),
                  make_rsrc(p.Wc + (size_t)n0 * row + skip, (uint64_t)min(BN, p.n - n0) * row - skip), row, row,
                  row - skip, s1 - s0};
-  const Scales sc{p.As + (size_t)s0 * cells * 64, p.Ws, cells, nb * blocks, n0 / 128 * blocks + s0, 1, blocks, nb - n0 / 128};
+  const Scales sc{p.As + (size_t)s0 * cells * 64, p.Ws, cells, n0 / 128 * blocks + s0, 1, blocks, nb - n0 / 128};
   typename Core::Acc acc;
   Core::run(t, sc, m0, smem, acc);
   if constexpr (SPLIT)
@@ -377,7 +364,7 @@ __global__ __launch_bounds__(NT) void lora_fp8_bwd_kernel(Fp8Product p) {
   const uint32_t arow = (uint32_t)stages * 128, brow = (uint32_t)kb * 128;
   const NnTile t{make_rsrc(p.Ac + (size_t)m0 * arow, (uint64_t)min(BM, p.m - m0) * arow), arow,
                  reinterpret_cast<const char*>(p.Wc) + l0, brow, (uint64_t)p.n * brow - l0, stages};
-  const Scales sc{p.As, p.Ws, (p.m + 63) / 64, stages * kb, l0 / 128, kb, 1, kb - l0 / 128};
+  const Scales sc{p.As, p.Ws, (p.m + 63) / 64, l0 / 128, kb, 1, kb - l0 / 128};
   typename Core::Acc acc;
   const int s0 = (int)((int64_t)stages * split / p.splits), s1 = (int)((int64_t)stages * (split + 1) / p.splits);
   Core::run(t, sc, m0, s0, s1, smem, acc);
@@ -449,7 +436,7 @@ static hipError_t run_join(const Fp8Plan& p, const Fp8Product& q, int cols, hipS
 }
 template <int TG, int D>
 static hipError_t run_few(const Fp8Plan& p, const Fp8Product& q, hipStream_t st) {
-  hipLaunchKernelGGL((lora_fp8_few_kernel<TG, 1, D>), dim3((unsigned)p.grid), dim3(512), 0, st, q);
+  hipLaunchKernelGGL((lora_fp8_few_kernel<TG, D>), dim3((unsigned)p.grid), dim3(512), 0, st, q);
   return hipGetLastError();
 }
 template <int KS>

@@ -90,7 +90,6 @@ struct Scales {
   const uint8_t* a;
   const uint8_t* b;
   int cells;      // 64-row cells of A
-  int b_blocks;   // scale bytes of B
   int b_first;    // B: byte of (this tile's first column block, stage 0)
   int b_step;     // from stage to stage
   int b_col;      // from column block to column block

@@ -136,13 +136,13 @@ inline double split_time(const Fp8Plan& p, const TileCost& t) {
 // The one launch up to 2^14 values of X: each workgroup quantises all of them (1 x 4096
 // x 4096 6.2 us against 2.4 + 5.0 in two launches, 4 x 4096 x 4096 7.0 against 2.4 +
 // 5.5; 8 x 4096 x 4096 8.5 against 2.4 + 5.8).  Its LDS: X's codes and scales, the waves'
-// sums.
+// sums, 27 KB at most.
 constexpr int kFp8TokenRows = 16;
 inline size_t fp8_token_lds(int64_t m, int64_t k) { return (size_t)((m * fp8_blocks(k) * 129 + 15) / 16 * 16 + 8192); }
 
 inline Fp8Plan plan_fp8_fwd(int64_t m, int64_t n, int64_t k) {
   const int64_t groups = cdiv(n, 16);
-  if (m <= kFp8TokenRows && m * k <= (1 << 14) && fp8_token_lds(m, k) <= 160 * 1024) {
+  if (m <= kFp8TokenRows && m * k <= (1 << 14)) {
     // eight waves share a group of 16 features up to 1024 groups, else two (us: 1 x 11008
     // x 4096 10.9 and 12.3, 1 x 32000 x 4096 22.7 and 20.4, 1 x 4096 x 11008 12.4 and 27)
     const bool eight = groups <= 1024;
