@@ -583,7 +583,9 @@ lora_status lora_dropout(const void* X, const void* residual, void* Y, lora_dtyp
  * vocab at most 2^20, k at most 2^16, rows k at most 2^30 (LORA_ERR_UNSUPPORTED).
  *
  * lora_linear_xent_step: loss and gradients in one call, for a dloss known
- * beforehand; without dW it forms the logits once.
+ * beforehand; without dW it forms the logits once, and divides sums of e^(z - r) W with
+ * z - r up to 44 by the row's sum at the end, so that entries of W above 2^44 in size may
+ * pass fp32's range there.
  */
 size_t lora_linear_xent_workspace_size(int64_t rows, int64_t vocab, int64_t k, int dx, int dw);
 lora_status lora_linear_xent_fwd(const lora_bf16* X, const lora_bf16* W, const int32_t* labels, float* loss, float* saved,

@@ -676,7 +676,7 @@ def lora_linear_fp8_fwd(X, W_codes, W_scales, Y, workspace, stream=None) -> None
     way.
 
     X [m,k], Y [m,n]: torch.bfloat16; workspace: a device tensor of at least
-    lora_linear_fp8_fwd_workspace_size(m, n, k) bytes."""
+    lora_linear_fp8_fwd_workspace_size(m, n, k) bytes, which serve every smaller m too."""
     if _BF16 is None:
         _bind_torch()
     m, k = X.shape
@@ -697,7 +697,7 @@ def lora_linear_fp8_bwd(dY, W_codes, W_scales, dX, workspace, stream=None) -> No
     """dX = Q(dY) Q(W), the gradient of lora_linear_fp8_fwd's X, dY quantised on the way.
 
     dY [m,n], dX [m,k]: torch.bfloat16; workspace: a device tensor of at least
-    lora_linear_fp8_bwd_workspace_size(m, n, k) bytes."""
+    lora_linear_fp8_bwd_workspace_size(m, n, k) bytes, which serve every smaller m too."""
     if _BF16 is None:
         _bind_torch()
     m, n = dY.shape
@@ -716,8 +716,8 @@ def lora_linear_fp8_bwd(dY, W_codes, W_scales, dX, workspace, stream=None) -> No
 
 def lora_dropout(X, Y, seed: int, offset: int, p: float, residual=None, stream=None) -> None:
     """Y = residual + keep X / (1 - p), keep drawn from (seed, offset) wherever it is
-    needed (see include/lora_linear.h): element e of the tensor has the bit that
-    lora_dropout_keep_mask gives it.  The call uses ceil(numel / 16) counters from
+    needed (see include/lora_linear.h): where rows are whole multiples of 8 elements,
+    element e of the tensor has the bit that lora_dropout_keep_mask gives it.  The call uses ceil(numel / 16) counters from
     `offset` on; the gradient is the same call on dY without the residual.
 
     X, Y, residual: tensors of one shape, torch.bfloat16 or torch.float32; Y may be X
@@ -765,7 +765,7 @@ def lora_linear_xent_fwd(X, W, labels, loss, saved, workspace, stream=None) -> N
     X [rows,k], W [vocab,k]: torch.bfloat16; labels [rows]: torch.int32, one outside
     the vocabulary (-100, for instance) is none; loss [rows], saved [rows,2] (or None):
     torch.float32; workspace: a device tensor of at least
-    lora_linear_xent_workspace_size(rows, vocab, k) bytes."""
+    lora_linear_xent_workspace_size(rows, vocab, k) bytes, which serve fewer rows too."""
     rows, vocab, k = _check_xent(X, W, labels)
     _check_rows((loss, "loss", _F32, (rows,)))
     if saved is not None:

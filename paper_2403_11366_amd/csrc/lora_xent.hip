@@ -37,10 +37,10 @@
 // more than fp32's exponents: a masked tile at -1e10 made its row's sum infinite.)
 //
 // What bounds it: with many rows the two (with dW four) products, on the matrix cores --
-// loss and dX of 4096 rows, vocabulary 32000, k 4096 in 1.56 ms, the two products alone
+// loss and dX of 4096 rows, vocabulary 32000, k 4096 in 1.58 ms, the two products alone
 // 1.56 ms at the rate of a library's product of that size; a piece's logits 200 us, its
 // part of dX 204 us, 75% of the busy compute units' cycles multiplying.  With few rows the
-// bytes of W, read once for the logits and once for dX: 37 rows 122 us, of which the two
+// bytes of W, read once for the logits and once for dX: 37 rows 124 us, of which the two
 // reads of 262 MB take 42 and 50 us (6.3 and 5.2 TB/s).  A second reading from the
 // last-level cache was tried, in pieces that fit it: a launch for each piece cost more
 // than the cache's rate gave.
