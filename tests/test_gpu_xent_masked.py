@@ -61,3 +61,19 @@ def test_masked_first_part_beside_rows_that_are_not():
         loss, dX, _ = run(x, w, labels, d, how)
         close((loss[~free], dX[~free][:, 1:], None), (want[0], want[1][:, 1:], None), (tol[0], tol[1][:, 1:], None), how)
         close((loss[free], dX[free][:, 1:], None), (want_f[0], want_f[1][:, 1:], None), (tol_f[0], tol_f[1][:, 1:], None), how)
+
+
+@pytest.mark.parametrize("rows,vocab,k", [(1, 300, 8), (40, 6000, 72), (300, 1500, 64), (4100, 20011, 72)])
+@pytest.mark.parametrize("fill", [0xFF80, 0xFF7F, 0xE2AD, 0xD015])
+@pytest.mark.parametrize("level", [-300.0, 0.0, 300.0])
+def test_the_label_alone_is_left(rows, vocab, k, fill, level):
+    """Every column but the label's masked, by minus infinity, the lowest value, -1.6e21 or
+    -1e10: probability 1, so that loss and gradients are 0."""
+    print(f"xent label alone {rows} x {vocab} x {k}, mask {fill:#x}, near {level}", flush=True)
+    x, w, labels, d = masked(rows, vocab, k, vocab - 1, fill, level)
+    known = (labels >= 0) & (labels < vocab)
+    assert (labels[known] == vocab - 1).all()
+    for how, dw in (("step", False), ("step", True), ("two", True)):
+        loss, dX, dW = run(x, w, labels, d, how, True, dw)
+        assert (loss == 0).all() and (dX[:, 1:] == 0).all(), how
+        assert not dw or (dW == 0).all(), how
